@@ -17,6 +17,9 @@
  *   espo_advantages_packed    both for trajectories stored back to back, without padding
  *   espo_batch_stats  update of the frozen statistics and of beta between batches (Section 4.2, 4.3)
  *   espo_whiten       whitening of the advantages over the valid tokens (standard PPO step)
+ * and, on the logits of the policy update:
+ *   espo_logprobs     log-probabilities of given tokens and the entropy, and their backward pass
+ *   espo_policy_loss  the clipped objective (Eq. ppo) with its gradient on the logits
  *
  * Conventions for every entry point
  *   - "device" pointers are HIP device memory owned by the caller; the library
@@ -480,6 +483,92 @@ size_t espo_advantages_ws_bytes(int64_t B);
 
 /* lengths: device [B] int32; order: device [B] int32 out.  B, T >= 0 (B = 0 is a no-op), T < 2^31, B < 2^30. */
 int espo_length_order(const int32_t* lengths, int64_t B, int64_t T, int32_t* order, void* stream);
+
+/*
+ * espo_logprobs, espo_logprobs_backward -- log-probabilities of given tokens under the policy that is being
+ * updated, the entropy, and the gradient of both on the logits (the ratio of Eq. ppo needs the first, an entropy
+ * bonus the second).  Rows are tokens of the batch: row n is one position with its V logits.  With
+ * t_v = (x_v - max x) / temperature, S = sum_v exp t_v and pi_v = exp(t_v) / S:
+ *   logprob[n] = t_a - ln S for a = tokens[n],       entropy[n] = ln S - sum_v pi_v t_v,
+ *   dlogits[n,v] = (g ([v = a] - pi_v) - h pi_v (ln pi_v + entropy[n])) / temperature
+ * where g = dlogprob[n] and h = dentropy[n] are the loss's derivatives.  The sums are fp32; a gradient is rounded to the
+ * logits' type once, as it is stored.
+ * A row whose token is outside [0, V) is not used (padding, a prompt): its logits are not read, logprob and entropy
+ * are 0 and its gradient is 0.  Masked logits (at or below -1e30) have probability and gradient 0; a token that is
+ * masked itself has logprob -inf.  NaN and +inf are not supported in rows that are used (results for that row are
+ * unspecified, no fault).
+ *
+ * Arguments
+ *   logits      device, [N, row_stride] elements of `dt`, base and row pitch in bytes multiples of 16, as for espo_step.
+ *   N, V        N >= 0 (0 is a no-op), V >= 1; N < 2^31, V <= 2^30, and for the gradient N * ceil(V / 8192) < 2^31
+ *               (bf16; V / 4096 for fp32) (ESPO_ERANGE).
+ *   row_stride  elements between rows, >= V.
+ *   temperature between 1e-30 and 1e26.
+ *   tokens      device, [N] int32.
+ *   logprob     device, [N] fp32 out.
+ *   entropy     device, [N] fp32 out, may be NULL (then nothing is spent on it).  For espo_logprobs_backward an input,
+ *               which only has to be there with `dentropy`.
+ *   stats       device, [N][2] fp32 out, 8-byte aligned, may be NULL: max x and S of every row, for espo_logprobs_backward.
+ *   dlogprob    device, [N] fp32;  dentropy  device, [N] fp32 or NULL.
+ *   dlogits     device, [N, grad_stride] of `dt`, base and row pitch multiples of 16 bytes; only the first V of each row are written.
+ *               May be `logits` itself with grad_stride = row_stride (the gradient then replaces the logits); no other overlap.
+ *   stream      hipStream_t as void*.
+ */
+int espo_logprobs(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
+                  const int32_t* tokens, float* logprob, float* entropy, float* stats,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+int espo_logprobs_backward(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
+                           const int32_t* tokens, const float* stats, const float* entropy,
+                           const float* dlogprob, const float* dentropy, void* dlogits, int64_t grad_stride, void* stream);
+
+/* Bytes of workspace for espo_logprobs (0 where it needs none). */
+size_t espo_logprobs_workspace_bytes(int64_t N, int64_t V, espo_dtype dt);
+
+/*
+ * espo_policy_loss -- the clipped objective of the policy update (Section 3, Eq. ppo) with an optional entropy bonus, and
+ * its gradient on the logits.  For every used row n (see espo_logprobs) with A = adv[n], w = scale * weights[n] and
+ * r = exp(logprob[n] - old_logprob[n]):
+ *   loss = sum_n w (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) - entropy_coef * entropy[n])
+ *   d(loss)/d(logprob[n]) = -w r A, or 0 where the clipped product is the smaller one (A >= 0 and r > 1 + clip_high, or A < 0 and
+ *   r < 1 - clip_low); d(loss)/d(entropy[n]) = -w entropy_coef; on the logits as in espo_logprobs_backward.
+ * A mean over the valid tokens is scale = 1 / their number (or weights that say otherwise, one per token).  old_logprob is what
+ * espo_step or espo_logprobs returned when the tokens were drawn, adv what espo_whiten returned, both in the order of the rows.
+ * The exponent of r is held at 88 at most (e^88 is the largest power of e in fp32).
+ *
+ * Arguments as for espo_logprobs, and
+ *   old_logprob, adv   device, [N] fp32; read for used rows only.
+ *   weights     device, [N] fp32, or NULL for 1.
+ *   ctrl        host, read during the call: 0 <= clip_low <= 1, clip_high >= 0, finite entropy_coef and scale.
+ *   dlogits, grad_stride   as for espo_logprobs_backward (logits may be overwritten), or NULL for the loss alone.
+ *   logprob, entropy   device, [N] fp32 out, either may be NULL.
+ *   out         device, one espo_policy_result, 8-byte aligned: sums over the used rows, formed in double in a fixed order and
+ *               rounded once.
+ *   workspace   device scratch of at least espo_policy_loss_workspace_bytes(N, V, dt) bytes, 16-byte aligned; contents before and
+ *               after the call are irrelevant.
+ */
+typedef struct {
+  float clip_low, clip_high; /* the ratio is clipped to [1 - clip_low, 1 + clip_high] */
+  float entropy_coef;        /* weight of the entropy bonus, 0 = none */
+  float scale;               /* common weight of all rows */
+} espo_policy_ctrl;
+
+typedef struct {
+  float loss;       /* the objective */
+  float policy;     /* its part without the bonus */
+  float entropy;    /* sum w entropy */
+  float kl;         /* sum w (r - 1 - ln r), an estimate of the divergence from the old policy */
+  float clipped;    /* sum w over the rows that are clipped */
+  int32_t reserved;
+  int64_t tokens;   /* used rows */
+} espo_policy_result;
+
+int espo_policy_loss(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
+                     const int32_t* tokens, const float* old_logprob, const float* adv, const float* weights,
+                     const espo_policy_ctrl* ctrl, void* dlogits, int64_t grad_stride, float* logprob, float* entropy,
+                     espo_policy_result* out, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t espo_policy_loss_workspace_bytes(int64_t N, int64_t V, espo_dtype dt);
 
 /* Static, human-readable text for a status code (never NULL). */
 const char* espo_strerror(int code);

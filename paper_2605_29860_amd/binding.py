@@ -75,6 +75,18 @@ class _BatchResult(C.Structure):
 BATCH_RESULT_BYTES = C.sizeof(_BatchResult)
 
 
+class _PolicyCtrl(C.Structure):
+    _fields_ = [("clip_low", C.c_float), ("clip_high", C.c_float), ("entropy_coef", C.c_float), ("scale", C.c_float)]
+
+
+class _PolicyResult(C.Structure):
+    _fields_ = [("loss", C.c_float), ("policy", C.c_float), ("entropy", C.c_float), ("kl", C.c_float), ("clipped", C.c_float),
+                ("reserved", C.c_int32), ("tokens", C.c_int64)]
+
+
+POLICY_RESULT_BYTES = C.sizeof(_PolicyResult)
+
+
 def load_library():
     """Loads libespo.so (built in-tree by `build.py`); raises if it is not there."""
     global _lib
@@ -131,6 +143,17 @@ def load_library():
         lib.espo_batch_stats_static.argtypes = [vp, vp, vp, i64, i64, f32, f32, f32, C.POINTER(_BatchCtrl), vp, vp]
         lib.espo_batch_stats_workspace_bytes.restype = sz
         lib.espo_batch_stats_workspace_bytes.argtypes = [i64, i64]
+        lib.espo_logprobs.restype = C.c_int
+        lib.espo_logprobs.argtypes = [vp, C.c_int, i64, i64, i64, f32, vp, vp, vp, vp, vp, sz, vp]
+        lib.espo_logprobs_backward.restype = C.c_int
+        lib.espo_logprobs_backward.argtypes = [vp, C.c_int, i64, i64, i64, f32, vp, vp, vp, vp, vp, vp, i64, vp]
+        lib.espo_logprobs_workspace_bytes.restype = sz
+        lib.espo_logprobs_workspace_bytes.argtypes = [i64, i64, C.c_int]
+        lib.espo_policy_loss.restype = C.c_int
+        lib.espo_policy_loss.argtypes = [vp, C.c_int, i64, i64, i64, f32, vp, vp, vp, vp, C.POINTER(_PolicyCtrl), vp, i64, vp, vp, vp,
+                                         vp, sz, vp]
+        lib.espo_policy_loss_workspace_bytes.restype = sz
+        lib.espo_policy_loss_workspace_bytes.argtypes = [i64, i64, C.c_int]
         lib.espo_debug_copy.restype = C.c_int
         lib.espo_debug_copy.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         _lib = lib
@@ -511,3 +534,106 @@ def espo_advantages_terminal_ws(values: torch.Tensor, lengths: torch.Tensor, sto
                 dev(adv, torch.float32, "adv", None, shape), dev(returns, torch.float32, "returns", None, shape),
                 dev(order, torch.int32, "order", B, None), dev(workspace, torch.uint8, "workspace", None, None),
                 workspace.numel() if workspace is not None else 0, _stream(stream)))
+
+
+def _logits_dtype(t: torch.Tensor) -> int:
+    if t.dtype == torch.bfloat16:
+        return ESPO_BF16
+    if t.dtype == torch.float32:
+        return ESPO_F32
+    raise TypeError("logits must be bfloat16 or float32")
+
+
+def _rows(t: torch.Tensor, name: str, V: int | None):
+    """Address, rows, vocabulary and row stride of a tensor of logits [rows, row_stride] (a view of fewer columns too)."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1) or not _on_gpu(t):
+        raise TypeError(f"{name}: need a 2-D GPU tensor with unit stride along the vocabulary")
+    if t.is_cuda and t.get_device() != _current_device():
+        raise ValueError(f"{name}: on device {t.get_device()}, which is not the current one")
+    N, width = t.shape
+    V = width if V is None else int(V)
+    if V > width:
+        raise EspoError(-1, f"V exceeds the width of {name}")
+    stride = t.stride(0)
+    if N <= 1:                                    # torch may give any stride to a single row
+        stride = -(-width * t.element_size() // 16) * 16 // t.element_size()
+    return t.data_ptr(), N, V, stride
+
+
+def _gradient(t: torch.Tensor, logits: torch.Tensor, V: int):
+    """Address and row stride of the tensor that the gradient on `logits` is written to."""
+    if t.dtype != logits.dtype:
+        raise TypeError(f"dlogits: need the type of logits, {logits.dtype}")
+    ptr, N, _, stride = _rows(t, "dlogits", V)
+    if N != logits.shape[0]:
+        raise ValueError(f"dlogits: need {logits.shape[0]} rows, got {N}")
+    return ptr, stride
+
+
+def espo_logprobs_workspace_bytes(N: int, V: int, dtype: torch.dtype) -> int:
+    return int(load_library().espo_logprobs_workspace_bytes(N, V, ESPO_BF16 if dtype == torch.bfloat16 else ESPO_F32))
+
+
+def espo_logprobs(logits: torch.Tensor, temperature: float, tokens: torch.Tensor, logprob: torch.Tensor,
+                  entropy: torch.Tensor | None = None, stats: torch.Tensor | None = None, V: int | None = None,
+                  workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Log-probabilities of `tokens` [N] under `logits` [N, row_stride], and on request the entropy and what
+    `espo_logprobs_backward` needs (`stats` [N, 2]); see `espo_logprobs` in include/espo.h."""
+    lib = load_library()
+    dev = _checker(lib)
+    dt = _logits_dtype(logits)
+    ptr, N, V, stride = _rows(logits, "logits", V)
+    call = _entry(lib, "espo_logprobs")
+    _check(call(ptr, dt, N, V, stride, float(temperature), dev(tokens, torch.int32, "tokens", N, None),
+                dev(logprob, torch.float32, "logprob", N, None), dev(entropy, torch.float32, "entropy", N, None),
+                dev(stats, torch.float32, "stats", 2 * N, None), dev(workspace, torch.uint8, "workspace", None, None),
+                workspace.numel() if workspace is not None else 0, _stream(stream)))
+
+
+def espo_logprobs_backward(logits: torch.Tensor, temperature: float, tokens: torch.Tensor, stats: torch.Tensor,
+                           dlogprob: torch.Tensor, dlogits: torch.Tensor, entropy: torch.Tensor | None = None,
+                           dentropy: torch.Tensor | None = None, V: int | None = None, stream=None) -> None:
+    """Gradient on the logits from those on the log-probabilities and the entropy (`dentropy` needs the forward pass's
+    `entropy`); `dlogits` may be `logits`.  See `espo_logprobs_backward` in include/espo.h."""
+    lib = load_library()
+    dev = _checker(lib)
+    dt = _logits_dtype(logits)
+    ptr, N, V, stride = _rows(logits, "logits", V)
+    grad, grad_stride = _gradient(dlogits, logits, V)
+    call = _entry(lib, "espo_logprobs_backward")
+    _check(call(ptr, dt, N, V, stride, float(temperature), dev(tokens, torch.int32, "tokens", N, None),
+                dev(stats, torch.float32, "stats", 2 * N, None), dev(entropy, torch.float32, "entropy", N, None),
+                dev(dlogprob, torch.float32, "dlogprob", N, None), dev(dentropy, torch.float32, "dentropy", N, None),
+                grad, grad_stride, _stream(stream)))
+
+
+def espo_policy_loss_workspace_bytes(N: int, V: int, dtype: torch.dtype) -> int:
+    return int(load_library().espo_policy_loss_workspace_bytes(N, V, ESPO_BF16 if dtype == torch.bfloat16 else ESPO_F32))
+
+
+def espo_policy_loss(logits: torch.Tensor, temperature: float, tokens: torch.Tensor, old_logprob: torch.Tensor, adv: torch.Tensor,
+                     out: torch.Tensor, workspace: torch.Tensor, dlogits: torch.Tensor | None = None,
+                     logprob: torch.Tensor | None = None, entropy: torch.Tensor | None = None, weights: torch.Tensor | None = None,
+                     clip_low: float = 0.2, clip_high: float = 0.2, entropy_coef: float = 0.0, scale: float = 1.0,
+                     V: int | None = None, stream=None) -> None:
+    """The clipped objective and its gradient on the logits (`dlogits`, which may be `logits`, or None for the loss alone); see
+    `espo_policy_loss` in include/espo.h.  `out`: uint8 GPU tensor of POLICY_RESULT_BYTES bytes (decode a host copy with
+    `read_policy_result`); `workspace`: uint8 GPU tensor of `espo_policy_loss_workspace_bytes` bytes."""
+    lib = load_library()
+    dev = _checker(lib)
+    dt = _logits_dtype(logits)
+    ptr, N, V, stride = _rows(logits, "logits", V)
+    grad, grad_stride = (None, 0) if dlogits is None else _gradient(dlogits, logits, V)
+    ctrl = _PolicyCtrl(clip_low, clip_high, entropy_coef, scale)
+    call = _entry(lib, "espo_policy_loss")
+    _check(call(ptr, dt, N, V, stride, float(temperature), dev(tokens, torch.int32, "tokens", N, None),
+                dev(old_logprob, torch.float32, "old_logprob", N, None), dev(adv, torch.float32, "adv", N, None),
+                dev(weights, torch.float32, "weights", N, None), ctrl, grad, grad_stride, dev(logprob, torch.float32, "logprob", N, None),
+                dev(entropy, torch.float32, "entropy", N, None), dev(out, torch.uint8, "out", POLICY_RESULT_BYTES, None),
+                dev(workspace, torch.uint8, "workspace", None, None), workspace.numel() if workspace is not None else 0, _stream(stream)))
+
+
+def read_policy_result(out: torch.Tensor) -> dict:
+    """Host view of an espo_policy_result that `espo_policy_loss` wrote (synchronises through the copy)."""
+    r = _PolicyResult.from_buffer_copy(bytes(out.cpu().numpy().tobytes()[:POLICY_RESULT_BYTES]))
+    return {name: getattr(r, name) for name, _ in _PolicyResult._fields_ if name != "reserved"}

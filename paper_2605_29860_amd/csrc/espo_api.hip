@@ -115,12 +115,33 @@ int step_checked(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_
                            stop_step, tokens, regret, logprob, entropy, workspace, plan, (hipStream_t)stream);
 }
 
+// Checks that the operators on rows of logits with given tokens share; ESPO_OK means "go on".
+int rows_checked(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens) {
+  if (dt != ESPO_F32 && dt != ESPO_BF16) return ESPO_EINVAL;
+  if (N < 0 || V < 1 || row_stride < V) return ESPO_EINVAL;
+  if (!(temperature >= 1e-30f && temperature <= 1e26f)) return ESPO_EINVAL;  // log2(e) / T and its product with -1e30 stay fp32 numbers
+  if (N == 0) return ESPO_OK;
+  if (!logits || !tokens) return ESPO_EINVAL;
+  if (N > 0x7fffffff || V > (1 << 30)) return ESPO_ERANGE;
+  if (!aligned16(logits) || ((size_t)row_stride * (dt == ESPO_BF16 ? 2 : 4)) % 16 != 0) return ESPO_EALIGN;
+  return ESPO_OK;
+}
+
+// The same for the gradient that they write.
+int grad_checked(espo_dtype dt, int64_t N, int64_t V, const void* logits, int64_t row_stride, const void* dlogits, int64_t grad_stride) {
+  if (grad_stride < V) return ESPO_EINVAL;
+  if (dlogits == logits && grad_stride != row_stride) return ESPO_EINVAL;  // in place: the same rows
+  if (!espo::grad_indexable(dt, N, V)) return ESPO_ERANGE;
+  if (!aligned16(dlogits) || ((size_t)grad_stride * (dt == ESPO_BF16 ? 2 : 4)) % 16 != 0) return ESPO_EALIGN;
+  return ESPO_OK;
+}
+
 }  // namespace
 
 #pragma GCC visibility push(default)
 extern "C" {
 
-int espo_version(void) { return 330; }
+int espo_version(void) { return 400; }
 
 int espo_debug_step(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_t row_stride, float temperature,
                     uint64_t seed, int32_t step, const float* values, const espo_params* params, float* z, uint8_t* alive,
@@ -369,6 +390,60 @@ int espo_advantages_packed(const float* rewards, const float* terminal_reward, c
     return ESPO_EALIGN;
   return espo::launch_advantages(rewards, terminal_reward, values, nullptr, cu_seqlens, N, stopped, B, 0, r_fail, gamma,
                                  lambda, 0, td, adv, returns, nullptr, nullptr, nullptr, nullptr, (hipStream_t)stream);
+}
+
+size_t espo_logprobs_workspace_bytes(int64_t N, int64_t V, espo_dtype dt) {
+  (void)N; (void)V; (void)dt;
+  return 0;
+}
+
+int espo_logprobs(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
+                  const int32_t* tokens, float* logprob, float* entropy, float* stats, void* workspace, size_t workspace_bytes,
+                  void* stream) {
+  (void)workspace; (void)workspace_bytes;
+  const int rc = rows_checked(logits, dt, N, V, row_stride, temperature, tokens);
+  if (rc != ESPO_OK || N == 0) return rc;
+  if (!logprob) return ESPO_EINVAL;
+  if (((uintptr_t)stats & 7u) != 0) return ESPO_EALIGN;
+  return espo::launch_logprobs(logits, dt, N, V, row_stride, temperature, tokens, logprob, entropy, stats, (hipStream_t)stream);
+}
+
+int espo_logprobs_backward(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
+                           const int32_t* tokens, const float* stats, const float* entropy, const float* dlogprob,
+                           const float* dentropy, void* dlogits, int64_t grad_stride, void* stream) {
+  int rc = rows_checked(logits, dt, N, V, row_stride, temperature, tokens);
+  if (rc != ESPO_OK || N == 0) return rc;
+  if (!stats || !dlogprob || !dlogits || (dentropy && !entropy)) return ESPO_EINVAL;
+  rc = grad_checked(dt, N, V, logits, row_stride, dlogits, grad_stride);
+  if (rc != ESPO_OK) return rc;
+  if (((uintptr_t)stats & 7u) != 0) return ESPO_EALIGN;
+  return espo::launch_logprobs_backward(logits, dt, N, V, row_stride, temperature, tokens, stats, entropy, dlogprob, dentropy, dlogits,
+                                        grad_stride, (hipStream_t)stream);
+}
+
+size_t espo_policy_loss_workspace_bytes(int64_t N, int64_t V, espo_dtype dt) {
+  if (N <= 0 || V < 1 || (dt != ESPO_F32 && dt != ESPO_BF16)) return 0;
+  return espo::policy_workspace(N);
+}
+
+int espo_policy_loss(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
+                     const int32_t* tokens, const float* old_logprob, const float* adv, const float* weights,
+                     const espo_policy_ctrl* ctrl, void* dlogits, int64_t grad_stride, float* logprob, float* entropy,
+                     espo_policy_result* out, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = rows_checked(logits, dt, N, V, row_stride, temperature, tokens);
+  if (rc != ESPO_OK) return rc;
+  if (!ctrl || !out) return ESPO_EINVAL;
+  if (!(ctrl->clip_low >= 0.0f && ctrl->clip_low <= 1.0f) || !(ctrl->clip_high >= 0.0f) || !isfinite(ctrl->clip_high)) return ESPO_EINVAL;
+  if (!isfinite(ctrl->entropy_coef) || !isfinite(ctrl->scale)) return ESPO_EINVAL;
+  if (N > 0 && (!old_logprob || !adv)) return ESPO_EINVAL;
+  if (N > 0 && dlogits) {
+    rc = grad_checked(dt, N, V, logits, row_stride, dlogits, grad_stride);
+    if (rc != ESPO_OK) return rc;
+  }
+  if (((uintptr_t)out & 7u) != 0) return ESPO_EALIGN;
+  if (N > 0 && (!workspace || workspace_bytes < espo::policy_workspace(N) || !aligned16(workspace))) return ESPO_EWORKSPACE;
+  return espo::launch_policy_loss(logits, dt, N, V, row_stride, temperature, tokens, old_logprob, adv, weights, *ctrl, dlogits,
+                                  grad_stride, logprob, entropy, out, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

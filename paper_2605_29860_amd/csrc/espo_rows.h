@@ -1,0 +1,152 @@
+// Device-side access to rows of logits, 16 bytes at a time, and the softmax sum of a row over one workgroup.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/espo.h"
+#include "espo_device.h"
+
+namespace espo {
+
+// Logits at or below this are masked like -inf, whatever they are filled with.
+constexpr float kMaskedRow = -1e30f;
+// Exponents (to base 2) are held above this where they are multiplied by their own power: 2^-200 is 0 in fp32, and so is the product.
+constexpr float kLeastExponent = -200.0f;
+
+template <int DT>
+constexpr int vec_elems() { return DT == ESPO_BF16 ? 8 : 4; }  // logits in 16 bytes
+template <int DT>
+constexpr int logit_bytes() { return DT == ESPO_BF16 ? 2 : 4; }
+
+template <int DT>
+__device__ __forceinline__ void vec_unpack(u32x4 r, float x[vec_elems<DT>()]) {
+  if constexpr (DT == ESPO_BF16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __builtin_bit_cast(float, r[i] << 16);
+      x[2 * i + 1] = __builtin_bit_cast(float, r[i] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = r[i];  // a vector's element as the operand of a bit cast is its element 0
+      x[i] = __builtin_bit_cast(float, w);
+    }
+  }
+}
+
+// Rounded once, to the nearest even.
+template <int DT>
+__device__ __forceinline__ u32x4 vec_pack(const float x[vec_elems<DT>()]) {
+  u32x4 r;
+  if constexpr (DT == ESPO_BF16) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, bf16x2));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, x[i]);
+  }
+  return r;
+}
+
+// The 16 bytes of a vector that holds no logit: all masked.
+template <int DT>
+__device__ __forceinline__ u32x4 vec_masked() {
+  constexpr uint32_t w = DT == ESPO_BF16 ? 0xFF80FF80u : 0xFF800000u;
+  return u32x4{w, w, w, w};
+}
+
+// Vector `i` of a row of V logits; what lies at or beyond V (a row's last 16 bytes) becomes masked.  Rows start at multiples of 16 bytes
+// and so do their pitches, so that the 16 bytes that a row ends in belong to the row's own pitch.
+template <int DT>
+__device__ __forceinline__ u32x4 vec_load(const char* row, uint32_t i, uint32_t V) {
+  constexpr uint32_t E = vec_elems<DT>();
+  if (i * E >= V) return vec_masked<DT>();
+  u32x4 r = __builtin_nontemporal_load((const u32x4*)(row + (size_t)i * 16));
+  const uint32_t in = V - i * E;
+  if (in < E) {
+#pragma unroll
+    for (uint32_t w = 0; w < 4; ++w) {
+      if constexpr (DT == ESPO_BF16) {
+        if (2 * w >= in) r[w] = 0xFF80FF80u;
+        else if (2 * w + 1 >= in) r[w] = (r[w] & 0xFFFFu) | 0xFF800000u;
+      } else {
+        if (w >= in) r[w] = 0xFF800000u;
+      }
+    }
+  }
+  return r;
+}
+
+// Stores vector `i`, and of a row's last one only what lies below V.
+template <int DT>
+__device__ __forceinline__ void vec_store(char* row, uint32_t i, uint32_t V, u32x4 r) {
+  constexpr uint32_t E = vec_elems<DT>();
+  if (i * E + E <= V) {
+    __builtin_nontemporal_store(r, (u32x4*)(row + (size_t)i * 16));
+    return;
+  }
+  for (uint32_t j = 0; i * E + j < V; ++j) {
+    if constexpr (DT == ESPO_BF16)
+      ((uint16_t*)row)[i * E + j] = (uint16_t)(r[j >> 1] >> (16 * (j & 1)));
+    else
+      ((uint32_t*)row)[i * E + j] = r[j];
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ float logit_at(const char* row, uint32_t v) {
+  if constexpr (DT == ESPO_BF16)
+    return __builtin_bit_cast(float, (uint32_t)((const uint16_t*)row)[v] << 16);
+  else
+    return ((const float*)row)[v];
+}
+
+// Softmax sums relative to the largest logit seen: s = sum 2^t, a = sum t 2^t with t = (x - m) k2, k2 = log2(e) / temperature.
+// The difference x - m is formed first: as x k2 - m k2 the rounding of m k2 would scale a lane's sums by a factor of its own.
+// m starts at kMaskedRow, and sums of a lane that has seen nothing above it are dropped when lanes are merged.
+struct SoftmaxSums {
+  float m, s, a;
+};
+
+template <bool kEntropy>
+__device__ __forceinline__ void rescale(SoftmaxSums& p, float m, float k2) {
+  const float d = fmaxf((p.m - m) * k2, kLeastExponent), f = __builtin_amdgcn_exp2f(d);
+  if constexpr (kEntropy) p.a = f * (p.a + d * p.s);
+  p.s *= f;
+  p.m = m;
+}
+
+template <bool kEntropy>
+__device__ __forceinline__ void add_logit(SoftmaxSums& p, float x, float k2) {
+  float t = (x - p.m) * k2;
+  if constexpr (kEntropy) t = fmaxf(t, kLeastExponent);
+  const float e = __builtin_amdgcn_exp2f(t);
+  p.s += e;
+  if constexpr (kEntropy) p.a += e * t;
+}
+
+// Merged over a wave, wave-uniform, in a fixed order.
+template <bool kEntropy>
+__device__ __forceinline__ SoftmaxSums wave_merge(SoftmaxSums p, float k2) {
+  const float m = wave_max(p.m);
+  if (!(p.m > kMaskedRow)) p.s = p.a = 0.0f;
+  rescale<kEntropy>(p, m, k2);
+  p.s = wave_sum(p.s);
+  if constexpr (kEntropy) p.a = wave_sum(p.a);
+  return p;
+}
+
+// Merged over a workgroup of W waves, the same in every thread; lds holds W entries, and a barrier has passed since its last use.
+template <int W, bool kEntropy>
+__device__ __forceinline__ SoftmaxSums block_merge(SoftmaxSums p, float k2, SoftmaxSums* lds) {
+  p = wave_merge<kEntropy>(p, k2);
+  const int lane = threadIdx.x & (kWave - 1);
+  if (lane == 0) lds[threadIdx.x >> 6] = p;
+  __syncthreads();
+  return wave_merge<kEntropy>(lane < W ? lds[lane] : SoftmaxSums{kMaskedRow, 0.0f, 0.0f}, k2);
+}
+
+}  // namespace espo

@@ -1,0 +1,139 @@
+"""Host-side contracts of the operators on rows of logits: what the C functions and the binding refuse (nothing is
+launched), and the 64-bit reference against automatic differentiation."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+import rows_reference as R
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import os
+    from paper_2605_29860_amd import binding, build
+    if not os.path.exists(binding.library_path()):
+        build.build_library()
+    return binding.load_library()
+
+
+FAKE, ODD = C.c_void_p(0x1000), C.c_void_p(0x1004)
+
+
+def test_logprobs_refusals(lib):
+    call = lambda logits=FAKE, dt=1, N=4, V=64, stride=64, T=1.0, tokens=FAKE, lp=FAKE, H=None, stats=None: lib.espo_logprobs(
+        logits, dt, N, V, stride, T, tokens, lp, H, stats, None, 0, None)
+    assert call(N=0) == 0 and call(N=0, logits=None, tokens=None) == 0
+    assert call(dt=2) == -1 and call(N=-1) == -1 and call(V=0) == -1 and call(stride=63) == -1
+    for T in (0.0, -1.0, math.nan, math.inf, 1e-31, 1e27):
+        assert call(T=T) == -1, T
+    assert call(logits=None) == -1 and call(tokens=None) == -1 and call(lp=None) == -1
+    assert call(logits=ODD) == -2 and call(V=63, stride=63) == -2 and call(stats=ODD) == -2
+    assert call(N=1 << 31) == -5 and call(V=(1 << 30) + 1, stride=1 << 31) == -5
+
+
+def test_logprobs_backward_refusals(lib):
+    call = lambda N=4, V=64, T=1.0, stats=FAKE, H=None, g=FAKE, h=None, d=C.c_void_p(0x2000), ds=64, logits=FAKE: lib.espo_logprobs_backward(
+        logits, 1, N, V, 64, T, FAKE, stats, H, g, h, d, ds, None)
+    assert call(N=0) == 0 and call(T=0.0) == -1
+    assert call(stats=None) == -1 and call(g=None) == -1 and call(d=None) == -1
+    assert call(h=FAKE) == -1                                # a gradient of the entropy needs the entropy
+    assert call(ds=63) == -1 and call(d=FAKE, ds=72) == -1   # in place with another pitch
+    assert call(d=ODD) == -2 and call(ds=65) == -2 and call(stats=ODD) == -2
+    big = lambda N: lib.espo_logprobs_backward(FAKE, 1, N, 8193, 8200, 1.0, FAKE, FAKE, None, FAKE, None, C.c_void_p(0x2000), 8200, None)
+    assert big(1 << 30) == -5                                # two workgroups a row
+
+
+def test_policy_loss_refusals(lib):
+    from paper_2605_29860_amd.binding import _PolicyCtrl
+    need = lib.espo_policy_loss_workspace_bytes(4, 64, 1)
+    assert need >= 4 * 16 and lib.espo_policy_loss_workspace_bytes(0, 64, 1) == 0 and lib.espo_policy_loss_workspace_bytes(4, 0, 1) == 0
+    ok = (0.2, 0.2, 0.0, 1.0)
+    call = lambda ctrl=ok, old=FAKE, adv=FAKE, d=C.c_void_p(0x2000), ds=64, out=FAKE, ws=FAKE, nws=need, T=1.0, null=False: lib.espo_policy_loss(
+        FAKE, 1, 4, 64, 64, T, FAKE, old, adv, None, None if null else C.byref(_PolicyCtrl(*ctrl)), d, ds, None, None, out, ws, nws, None)
+    assert call(null=True) == -1 and call(out=None) == -1 and call(old=None) == -1 and call(adv=None) == -1 and call(T=0.0) == -1
+    for bad in ((-0.1, 0.2, 0, 1), (1.1, 0.2, 0, 1), (0.2, -0.1, 0, 1), (0.2, math.inf, 0, 1), (math.nan, 0.2, 0, 1), (0.2, 0.2, math.nan, 1),
+                (0.2, 0.2, 0, math.inf)):
+        assert call(ctrl=bad) == -1, bad
+    assert call(d=ODD) == -2 and call(ds=32) == -1 and call(out=ODD) == -2
+    assert call(ws=None) == -3 and call(nws=need - 1) == -3 and call(ws=C.c_void_p(0x1008)) == -3
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    """The binding with a library that records its calls; host tensors stand in for device memory."""
+    from paper_2605_29860_amd import binding as b
+
+    class Recorder:
+        calls = []
+
+        def __getattr__(self, name):
+            return lambda *args: Recorder.calls.append((name, args)) or 0
+
+    Recorder.calls = []
+    monkeypatch.setattr(b, "load_library", lambda: Recorder())
+    monkeypatch.setattr(b, "_on_gpu", lambda t: True)
+    monkeypatch.setattr(b, "_stream", lambda s: None)
+    return b, Recorder.calls
+
+
+def test_binding_of_the_log_probabilities(recorder):
+    b, calls = recorder
+    N, V = 4, 64
+    f, i32 = lambda n: torch.zeros(n), lambda n: torch.zeros(n, dtype=torch.int32)
+    args = lambda **o: {**dict(logits=torch.zeros(N, V), temperature=1.0, tokens=i32(N), logprob=f(N), entropy=f(N), stats=f(2 * N)), **o}
+    b.espo_logprobs(**args())
+    back = lambda **o: {**dict(logits=torch.zeros(N, V), temperature=1.0, tokens=i32(N), stats=f(2 * N), dlogprob=f(N),
+                               dlogits=torch.zeros(N, V), entropy=f(N), dentropy=f(N)), **o}
+    b.espo_logprobs_backward(**back())
+    u8 = lambda n: torch.zeros(n, dtype=torch.uint8)
+    loss = lambda **o: {**dict(logits=torch.zeros(N, V), temperature=1.0, tokens=i32(N), old_logprob=f(N), adv=f(N), out=u8(b.POLICY_RESULT_BYTES),
+                               workspace=u8(64), dlogits=torch.zeros(N, V), logprob=f(N), entropy=f(N), weights=f(N)), **o}
+    b.espo_policy_loss(**loss())
+    assert len(calls) == 3
+    for fn, base, short in ((b.espo_logprobs, args, dict(tokens=i32(N - 1), logprob=f(N - 1), entropy=f(N - 1), stats=f(2 * N - 1))),
+                            (b.espo_logprobs_backward, back, dict(tokens=i32(N - 1), stats=f(2 * N - 1), dlogprob=f(N - 1), entropy=f(N - 1),
+                                                                  dentropy=f(N - 1), dlogits=torch.zeros(N - 1, V))),
+                            (b.espo_policy_loss, loss, dict(tokens=i32(N - 1), old_logprob=f(N - 1), adv=f(N - 1), out=u8(b.POLICY_RESULT_BYTES - 1),
+                                                            logprob=f(N - 1), entropy=f(N - 1), weights=f(N - 1)))):
+        for name, t in short.items():
+            with pytest.raises(ValueError, match=name):
+                fn(**base(**{name: t}))
+        with pytest.raises(TypeError):
+            fn(**base(logits=torch.zeros(N, V, dtype=torch.float16)))
+        with pytest.raises(TypeError):
+            fn(**base(logits=torch.zeros(V, N).t()))
+        with pytest.raises(TypeError):
+            fn(**base(tokens=torch.zeros(N, dtype=torch.int64)))
+        with pytest.raises(b.EspoError):
+            fn(**base(V=V + 1))
+    for fn, base in ((b.espo_logprobs_backward, back), (b.espo_policy_loss, loss)):
+        with pytest.raises(TypeError):
+            fn(**base(dlogits=torch.zeros(N, V, dtype=torch.bfloat16)))
+        with pytest.raises(b.EspoError):
+            fn(**base(dlogits=torch.zeros(N, V - 1)))
+    assert len(calls) == 3
+    # a row's pitch is the tensor's; a single row, whose stride means nothing, counts as whole 16 bytes
+    b.espo_logprobs(**args(logits=torch.zeros(N, 80)[:, :70]))
+    assert calls[-1][1][2:5] == (N, 70, 80)
+    b.espo_logprobs(**args(logits=torch.zeros(1, 70)))
+    assert calls[-1][1][2:5] == (1, 70, 72)
+
+
+def test_the_reference_against_automatic_differentiation():
+    g = torch.Generator().manual_seed(1)
+    N, V, T = 6, 23, 0.75
+    x = (torch.randn(N, V, generator=g, dtype=torch.float64) * 2).requires_grad_()
+    tokens = torch.randint(0, V, (N,), generator=g, dtype=torch.int32)
+    old, adv = torch.randn(N, generator=g).double() - 4, torch.randn(N, generator=g).double()
+    weights = torch.rand(N, generator=g).double()
+    logpi = torch.log_softmax(x / T, 1)
+    lp, H = logpi.gather(1, tokens[:, None].long())[:, 0], -(logpi.exp() * logpi).sum(1)
+    r = (lp - old).exp()
+    loss = (0.5 * weights * (-torch.minimum(r * adv, r.clamp(0.8, 1.3) * adv) - 0.1 * H)).sum()
+    loss.backward()
+    f = R.softmax_rows(x.detach(), T, tokens)
+    gg, h, sums, _ = R.policy_terms(f, old, adv, weights, 0.5, 0.2, 0.3, 0.1)
+    assert torch.allclose(R.logits_grad(f, gg, h), x.grad, rtol=1e-12, atol=1e-14)
+    assert torch.allclose(f["entropy"], H.detach(), rtol=1e-13) and float(sums[0]) == pytest.approx(float(loss.detach()), rel=1e-12)
