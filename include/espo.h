@@ -17,7 +17,8 @@
  *   espo_advantages_packed    both for trajectories stored back to back, without padding
  *   espo_batch_stats  update of the frozen statistics and of beta between batches (Section 4.2, 4.3)
  *   espo_whiten       whitening of the advantages over the valid tokens (standard PPO step)
- * and, on the logits of the policy update:
+ * and, on logits on their own:
+ *   espo_sample       a token per row from given random numbers, with settings per row
  *   espo_logprobs     log-probabilities of given tokens and the entropy, and their backward pass
  *   espo_policy_loss  the clipped objective (Eq. ppo) with its gradient on the logits
  *
@@ -483,6 +484,42 @@ size_t espo_advantages_ws_bytes(int64_t B);
 
 /* lengths: device [B] int32; order: device [B] int32 out.  B, T >= 0 (B = 0 is a no-op), T < 2^31, B < 2^30. */
 int espo_length_order(const int32_t* lengths, int64_t B, int64_t T, int32_t* order, void* stream);
+
+/*
+ * espo_sample -- one token per row from random numbers that the caller holds, every row with its own temperature and
+ * filters: what an evaluation or a serving program draws with.  (espo_step draws from its own random stream, with one
+ * setting for all rows.)  For row b with T = temperature[b], t_v = (x_v - max x) / T and w_v = exp t_v, a token is kept if
+ *   it is not masked (masked: x_v at or below -1e30),
+ *   top_k  fewer than top_k[b] tokens have a strictly larger logit (active for 0 < top_k[b] < V; ties at the k-th value are all kept),
+ *   top_p  of the tokens that top_k leaves, those with a strictly larger logit hold less than top_p[b] of their mass (active
+ *          for 0 < top_p[b] < 1; tokens of equal logit are kept or dropped together), and
+ *   min_p  w_v >= min(min_p[b], 1): its probability is at least min_p times the largest one (active for min_p[b] > 0).
+ * The most probable token is always kept.  With W = the sum of w over the kept tokens,
+ *   tokens[b]  = the lowest kept v whose sum of w over the kept indices up to and with v exceeds u[b] W,
+ *   logprob[b] = t_a - ln W, the logarithm of the probability it was drawn with.
+ * Weights and sums are double, so that the token is the definition's unless u[b] W lies within about 1e-13 W of one of the
+ * running sums.  u[b] in [0, 1); a larger one gives the last kept token, a smaller one the first.  T <= 0 is greedy: the lowest
+ * index of the largest logit, logprob 0.  A row whose logits are all masked, and one with alive[b] == 0, whose logits are
+ * not read, has token -1 and logprob 0.  NaN in logits or settings and +inf logits are not supported (results for that
+ * row are unspecified, no fault).
+ *
+ * Arguments
+ *   logits      device, [B, row_stride] elements of `dt`, base and row pitch in bytes multiples of 16, as for espo_step.
+ *   B, V        B >= 0 (0 is a no-op), V >= 1; B < 2^31, V <= 2^20 (ESPO_ERANGE).
+ *   row_stride  elements between rows, >= V.
+ *   temperature, top_p, min_p   device, [B] fp32;  top_k  device, [B] int32.  Each may be NULL: temperature 1, that filter off.
+ *   u           device, [B] fp32.
+ *   alive       device, [B] uint8, or NULL: every row is live.
+ *   tokens      device, [B] int32 out.
+ *   logprob     device, [B] fp32 out, may be NULL.
+ *   stream      hipStream_t as void*.
+ */
+int espo_sample(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_t row_stride, const float* temperature,
+                const int32_t* top_k, const float* top_p, const float* min_p, const float* u, const uint8_t* alive,
+                int32_t* tokens, float* logprob, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace for espo_sample (0 where it needs none). */
+size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
 
 /*
  * espo_logprobs, espo_logprobs_backward -- log-probabilities of given tokens under the policy that is being

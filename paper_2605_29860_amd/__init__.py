@@ -8,7 +8,8 @@ __all__ = ["espo_step", "espo_advantages", "espo_advantages_terminal", "espo_adv
            "load_library", "library_path", "espo_debug_step_workspace_bytes", "espo_debug_math_errors", "espo_debug_read", "espo_debug_sweep", "espo_debug_sweep_padded",
            "espo_debug_copy", "espo_batch_stats", "espo_batch_stats_workspace_bytes", "espo_batch_stats_static", "read_batch_result",
            "BATCH_RESULT_BYTES", "espo_logprobs", "espo_logprobs_backward", "espo_logprobs_workspace_bytes", "espo_policy_loss",
-           "espo_policy_loss_workspace_bytes", "read_policy_result", "POLICY_RESULT_BYTES"]
+           "espo_policy_loss_workspace_bytes", "read_policy_result", "POLICY_RESULT_BYTES", "espo_sample",
+           "espo_sample_workspace_bytes"]
 
 
 def __getattr__(name):

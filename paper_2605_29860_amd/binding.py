@@ -143,6 +143,10 @@ def load_library():
         lib.espo_batch_stats_static.argtypes = [vp, vp, vp, i64, i64, f32, f32, f32, C.POINTER(_BatchCtrl), vp, vp]
         lib.espo_batch_stats_workspace_bytes.restype = sz
         lib.espo_batch_stats_workspace_bytes.argtypes = [i64, i64]
+        lib.espo_sample.restype = C.c_int
+        lib.espo_sample.argtypes = [vp, C.c_int, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.espo_sample_workspace_bytes.restype = sz
+        lib.espo_sample_workspace_bytes.argtypes = [i64, i64, C.c_int]
         lib.espo_logprobs.restype = C.c_int
         lib.espo_logprobs.argtypes = [vp, C.c_int, i64, i64, i64, f32, vp, vp, vp, vp, vp, sz, vp]
         lib.espo_logprobs_backward.restype = C.c_int
@@ -568,6 +572,28 @@ def _gradient(t: torch.Tensor, logits: torch.Tensor, V: int):
     if N != logits.shape[0]:
         raise ValueError(f"dlogits: need {logits.shape[0]} rows, got {N}")
     return ptr, stride
+
+
+def espo_sample_workspace_bytes(B: int, V: int, dtype: torch.dtype) -> int:
+    return int(load_library().espo_sample_workspace_bytes(B, V, ESPO_BF16 if dtype == torch.bfloat16 else ESPO_F32))
+
+
+def espo_sample(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor, logprob: torch.Tensor | None = None,
+                temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None,
+                min_p: torch.Tensor | None = None, alive: torch.Tensor | None = None, V: int | None = None,
+                workspace: torch.Tensor | None = None, stream=None) -> None:
+    """One token per row of `logits` [B, row_stride] from the random numbers `u` [B], with settings per row ([B] each, or
+    None); see `espo_sample` in include/espo.h.  `workspace`: a uint8 GPU tensor of `espo_sample_workspace_bytes` bytes or None."""
+    lib = load_library()
+    dev = _checker(lib)
+    dt = _logits_dtype(logits)
+    ptr, B, V, stride = _rows(logits, "logits", V)
+    call = _entry(lib, "espo_sample")
+    _check(call(ptr, dt, B, V, stride, dev(temperature, torch.float32, "temperature", B, None), dev(top_k, torch.int32, "top_k", B, None),
+                dev(top_p, torch.float32, "top_p", B, None), dev(min_p, torch.float32, "min_p", B, None),
+                dev(u, torch.float32, "u", B, None), dev(alive, torch.uint8, "alive", B, None),
+                dev(tokens, torch.int32, "tokens", B, None), dev(logprob, torch.float32, "logprob", B, None),
+                dev(workspace, torch.uint8, "workspace", None, None), workspace.numel() if workspace is not None else 0, _stream(stream)))
 
 
 def espo_logprobs_workspace_bytes(N: int, V: int, dtype: torch.dtype) -> int:

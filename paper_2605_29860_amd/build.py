@@ -12,7 +12,7 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libespo.so")
 # translation units: source and its own flags (the step kernels take most of the time, so each logit type is one)
 SOURCES = [("espo_step.hip", []), ("espo_step.hip", ["-DESPO_STEP_F32"]), ("espo_advantages.hip", []), ("espo_whiten.hip", []),
-           ("espo_batch_stats.hip", []), ("espo_logprobs.hip", []), ("espo_api.hip", [])]
+           ("espo_batch_stats.hip", []), ("espo_logprobs.hip", []), ("espo_sample.hip", []), ("espo_api.hip", [])]
 # packed-fp32 VALU forms are switched off for every device translation unit
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

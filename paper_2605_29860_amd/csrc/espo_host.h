@@ -78,6 +78,10 @@ size_t advantages_workspace_layout(int64_t B, size_t* stats_offset, size_t* sort
 // The rows 0 .. B-1 ordered by clipped length, longest first (256 classes of length; one workgroup).
 int launch_length_order(const int32_t* lengths, int64_t B, int64_t T, int32_t* order, hipStream_t stream);
 
+int launch_sample(const void* logits, int dt, int64_t B, int64_t V, int64_t row_stride, const float* temperature, const int32_t* top_k,
+                  const float* top_p, const float* min_p, const float* u, const uint8_t* alive, int32_t* tokens, float* logprob,
+                  hipStream_t stream);
+
 // The policy update's operators.  stats: [N] pairs of row maximum and sum.
 int launch_logprobs(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,
                     float* logprob, float* entropy, float* stats, hipStream_t stream);

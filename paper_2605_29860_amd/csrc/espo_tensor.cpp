@@ -78,7 +78,7 @@ PyMethodDef entries[] = {ESPO_ENTRY(espo_step), ESPO_ENTRY(espo_debug_step), ESP
                          ESPO_ENTRY(espo_advantages_terminal), ESPO_ENTRY(espo_advantages_terminal_ws), ESPO_ENTRY(espo_advantages_packed),
                          ESPO_ENTRY(espo_length_order), ESPO_ENTRY(espo_whiten), ESPO_ENTRY(espo_whiten_from_ws),
                          ESPO_ENTRY(espo_batch_stats), ESPO_ENTRY(espo_batch_stats_static), ESPO_ENTRY(espo_logprobs),
-                         ESPO_ENTRY(espo_logprobs_backward), ESPO_ENTRY(espo_policy_loss)};
+                         ESPO_ENTRY(espo_logprobs_backward), ESPO_ENTRY(espo_policy_loss), ESPO_ENTRY(espo_sample)};
 
 // entry(name, address) -> the C function of that name at that address.
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t nargs) {

@@ -103,3 +103,32 @@ def policy_terms(f, old, adv, weights, scale, lo, hi, coef):
     sums = [(w * (-best - coef * f["entropy"])).sum(), (-w * best).sum(), (w * f["entropy"]).sum(), (w * (r - 1 - d)).sum(),
             (w * cut).sum()]
     return g, h, sums, dict(r=r, cut=cut, w=w, A=A, d=d)
+
+
+def sample_row(x, T, k, p, min_p, u):
+    """espo_sample's definition for one row: x [V] float64 on the CPU, settings as the kernel reads them (fp32 values).
+    Returns the token, its log-probability and how close u W comes to a running sum, relative to W."""
+    V, k = x.numel(), int(k)
+    index = torch.nonzero(x > MASKED)[:, 0]
+    if index.numel() == 0:
+        return -1, 0.0, 1.0
+    v = x[index]
+    if not T > 0:
+        return int(index[torch.nonzero(v == v.max())[0, 0]]), 0.0, 1.0
+    w = ((v - v.max()) / T).exp()
+    keep = torch.ones_like(v, dtype=torch.bool)
+    if 0 < k < V:
+        kth = torch.sort(v, descending=True).values[min(k, v.numel()) - 1]
+        keep &= v >= kth
+    if 0 < p < 1:
+        mass = torch.where(keep, w, 0.0)
+        levels, member = torch.unique(v, sorted=True, return_inverse=True)
+        per = torch.zeros_like(levels).index_add_(0, member, mass).flip(0)
+        above = per.cumsum(0) - per
+        keep &= (above < p * mass.sum()).flip(0)[member]
+    keep &= w >= min(min_p, 1.0)
+    index, v, w = index[keep], v[keep], w[keep]
+    upto = w.cumsum(0)
+    W = upto[-1]
+    i = min(int((upto <= u * W).sum()), index.numel() - 1)
+    return int(index[i]), float((v[i] - x.max()) / T - W.log()), float((upto - u * W).abs().min() / W)

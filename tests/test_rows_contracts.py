@@ -21,6 +21,16 @@ def lib():
 FAKE, ODD = C.c_void_p(0x1000), C.c_void_p(0x1004)
 
 
+def test_sample_refusals(lib):
+    call = lambda logits=FAKE, dt=1, B=4, V=64, stride=64, u=FAKE, tokens=FAKE: lib.espo_sample(
+        logits, dt, B, V, stride, None, None, None, None, u, None, tokens, None, None, 0, None)
+    assert call(B=0) == 0 and call(B=0, logits=None, u=None) == 0
+    assert call(dt=2) == -1 and call(B=-1) == -1 and call(V=0) == -1 and call(stride=63) == -1
+    assert call(logits=None) == -1 and call(u=None) == -1 and call(tokens=None) == -1
+    assert call(logits=ODD) == -2 and call(V=63, stride=63) == -2
+    assert call(B=1 << 31) == -5 and call(V=(1 << 20) + 1, stride=1 << 21) == -5
+
+
 def test_logprobs_refusals(lib):
     call = lambda logits=FAKE, dt=1, N=4, V=64, stride=64, T=1.0, tokens=FAKE, lp=FAKE, H=None, stats=None: lib.espo_logprobs(
         logits, dt, N, V, stride, T, tokens, lp, H, stats, None, 0, None)
@@ -119,6 +129,27 @@ def test_binding_of_the_log_probabilities(recorder):
     assert calls[-1][1][2:5] == (N, 70, 80)
     b.espo_logprobs(**args(logits=torch.zeros(1, 70)))
     assert calls[-1][1][2:5] == (1, 70, 72)
+
+
+def test_binding_of_the_draw(recorder):
+    b, calls = recorder
+    B, V = 4, 64
+    f = lambda n: torch.zeros(n)
+    args = lambda **o: {**dict(logits=torch.zeros(B, V), u=f(B), tokens=torch.zeros(B, dtype=torch.int32), logprob=f(B), temperature=f(B),
+                               top_k=torch.zeros(B, dtype=torch.int32), top_p=f(B), min_p=f(B), alive=torch.zeros(B, dtype=torch.uint8)), **o}
+    b.espo_sample(**args())
+    b.espo_sample(torch.zeros(B, V), f(B), torch.zeros(B, dtype=torch.int32))
+    assert len(calls) == 2 and calls[1][1][5:9] == (None,) * 4
+    for name in ("u", "tokens", "logprob", "temperature", "top_k", "top_p", "min_p", "alive"):
+        with pytest.raises(ValueError, match=name):
+            b.espo_sample(**args(**{name: args()[name][:B - 1]}))
+        with pytest.raises(TypeError, match=name):
+            b.espo_sample(**args(**{name: torch.zeros(B, dtype=torch.float64)}))
+    with pytest.raises(b.EspoError):
+        b.espo_sample(**args(V=V + 1))
+    with pytest.raises(TypeError):
+        b.espo_sample(**args(logits=torch.zeros(B, V, dtype=torch.float16)))
+    assert len(calls) == 2
 
 
 def test_the_reference_against_automatic_differentiation():
