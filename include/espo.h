@@ -498,14 +498,14 @@ int espo_length_order(const int32_t* lengths, int64_t B, int64_t T, int32_t* ord
  *   tokens[b]  = the lowest kept v whose sum of w over the kept indices up to and with v exceeds u[b] W,
  *   logprob[b] = t_a - ln W, the logarithm of the probability it was drawn with.
  * Weights and sums are double, so that the token is the definition's unless u[b] W lies within about 1e-13 W of one of the
- * running sums.  u[b] in [0, 1); a larger one gives the last kept token, a smaller one the first.  T <= 0 is greedy: the lowest
+ * running sums (weights below 1e-250 count as none).  u[b] in [0, 1); a larger one gives the last kept token, a smaller one the first.  T <= 0 is greedy: the lowest
  * index of the largest logit, logprob 0.  A row whose logits are all masked, and one with alive[b] == 0, whose logits are
  * not read, has token -1 and logprob 0.  NaN in logits or settings and +inf logits are not supported (results for that
  * row are unspecified, no fault).
  *
  * Arguments
  *   logits      device, [B, row_stride] elements of `dt`, base and row pitch in bytes multiples of 16, as for espo_step.
- *   B, V        B >= 0 (0 is a no-op), V >= 1; B < 2^31, V <= 2^20 (ESPO_ERANGE).
+ *   B, V        B >= 0 (0 is a no-op), V >= 1; B < 2^31, V <= 2^20, with any filter given V <= 2^19 (ESPO_ERANGE).
  *   row_stride  elements between rows, >= V.
  *   temperature, top_p, min_p   device, [B] fp32;  top_k  device, [B] int32.  Each may be NULL: temperature 1, that filter off.
  *   u           device, [B] fp32.

@@ -405,7 +405,7 @@ int espo_sample(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_t
   if (B < 0 || V < 1 || row_stride < V) return ESPO_EINVAL;
   if (B == 0) return ESPO_OK;
   if (!logits || !u || !tokens) return ESPO_EINVAL;
-  if (B > 0x7fffffff || V > (1 << 20)) return ESPO_ERANGE;
+  if (B > 0x7fffffff || V > (top_k || top_p || min_p ? 1 << 19 : 1 << 20)) return ESPO_ERANGE;  // a filter keeps the maxima of blocks in LDS
   if (!aligned16(logits) || ((size_t)row_stride * (dt == ESPO_BF16 ? 2 : 4)) % 16 != 0) return ESPO_EALIGN;
   return espo::launch_sample(logits, dt, B, V, row_stride, temperature, top_k, top_p, min_p, u, alive, tokens, logprob,
                              (hipStream_t)stream);

@@ -22,13 +22,15 @@ FAKE, ODD = C.c_void_p(0x1000), C.c_void_p(0x1004)
 
 
 def test_sample_refusals(lib):
-    call = lambda logits=FAKE, dt=1, B=4, V=64, stride=64, u=FAKE, tokens=FAKE: lib.espo_sample(
-        logits, dt, B, V, stride, None, None, None, None, u, None, tokens, None, None, 0, None)
+    call = lambda logits=FAKE, dt=1, B=4, V=64, stride=64, u=FAKE, tokens=FAKE, k=None, p=None, min_p=None: lib.espo_sample(
+        logits, dt, B, V, stride, None, k, p, min_p, u, None, tokens, None, None, 0, None)
     assert call(B=0) == 0 and call(B=0, logits=None, u=None) == 0
     assert call(dt=2) == -1 and call(B=-1) == -1 and call(V=0) == -1 and call(stride=63) == -1
     assert call(logits=None) == -1 and call(u=None) == -1 and call(tokens=None) == -1
     assert call(logits=ODD) == -2 and call(V=63, stride=63) == -2
     assert call(B=1 << 31) == -5 and call(V=(1 << 20) + 1, stride=1 << 21) == -5
+    for name in ("k", "p", "min_p"):
+        assert call(V=(1 << 19) + 1, stride=1 << 21, **{name: FAKE}) == -5
 
 
 def test_logprobs_refusals(lib):
