@@ -18,7 +18,6 @@ namespace espo {
 namespace {
 
 constexpr int kRowWaves = 8, kRowThreads = kRowWaves * kWave;
-constexpr int kRowLoads = 4;                     // 16-byte loads of a thread in flight
 constexpr int kGradThreads = 256, kGradLoads = 4;
 constexpr int kGradSpan = kGradThreads * kGradLoads;  // vectors of a workgroup
 constexpr int kSumThreads = 1024, kSumWaves = kSumThreads / kWave;
@@ -65,25 +64,29 @@ __global__ __launch_bounds__(kRowThreads) void espo_logprobs_kernel(RowArgs a, R
     return;
   }
   const char* x = a.logits + row * a.row_bytes;
-  const uint32_t nvec = (a.V + E - 1) / E;
+  const RowView r = row_view<DT>(x, a.V);
   SoftmaxSums p{kMaskedRow, 0.0f, 0.0f};
-  for (uint32_t base = 0; base < nvec; base += kRowThreads * kRowLoads) {
-    u32x4 r[kRowLoads];
+  stream_tiles(r, threadIdx.x >> 6, r.ntiles, kRowWaves, [&](uint32_t t, const u32x4* raw) {
+    float y[kAhead][E], m = p.m;
 #pragma unroll
-    for (int j = 0; j < kRowLoads; ++j) r[j] = vec_load<DT>(x, base + j * kRowThreads + threadIdx.x, a.V);
-    float y[kRowLoads][E], m = p.m;
+    for (int j = 0; j < kAhead; ++j) {
+      if (t + j * kRowWaves >= r.ntiles) {
 #pragma unroll
-    for (int j = 0; j < kRowLoads; ++j) {
-      vec_unpack<DT>(r[j], y[j]);
+        for (int i = 0; i < E; ++i) y[j][i] = kNegInf;
+        continue;
+      }
+      tile_logits<DT>(r, t + j * kRowWaves, raw[j], y[j]);
 #pragma unroll
       for (int i = 0; i < E; ++i) m = fmaxf(m, y[j][i]);
     }
     rescale<kEntropy>(p, m, a.k2);
 #pragma unroll
-    for (int j = 0; j < kRowLoads; ++j)
+    for (int j = 0; j < kAhead; ++j)
+      if (t + j * kRowWaves < r.ntiles) {
 #pragma unroll
-      for (int i = 0; i < E; ++i) add_logit<kEntropy>(p, y[j][i], a.k2);
-  }
+        for (int i = 0; i < E; ++i) add_logit<kEntropy>(p, y[j][i], a.k2);
+      }
+  });
   p = block_merge<kRowWaves, kEntropy>(p, a.k2, lds);
   if (threadIdx.x == 0) {
     float logprob, entropy;
@@ -112,6 +115,35 @@ __device__ __forceinline__ Surrogate surrogate(const PolicyArgs& q, int64_t row,
   c.weight = q.scale * (q.weights ? q.weights[row] : 1.0f);
   c.cut = adv >= 0.0f ? c.ratio > 1.0f + q.clip_high : c.ratio < 1.0f - q.clip_low;
   return c;
+}
+
+// A row's gradient: dx_v = 2^t (p0 + p1 t) with t = (x_v - m) k2, and `at` more at the token.
+struct RowGrad {
+  float m, p0, p1, at;
+};
+
+// m, s: the row's largest logit and sum; `entropy` only counts where h is not 0.
+__device__ __forceinline__ RowGrad row_grad(const RowArgs& a, float m, float s, float entropy, float g, float h) {
+  const float per = 1.0f / (a.temperature * s);
+  return RowGrad{m, -(h != 0.0f ? g + h * (entropy - logf(s)) : g) * per, -h * kLn2 * per, g / a.temperature};
+}
+
+template <int DT, bool kSlope>
+__device__ __forceinline__ u32x4 grad_vec(const RowArgs& a, const RowGrad& c, u32x4 raw, uint32_t i, int32_t token) {
+  constexpr int E = vec_elems<DT>();
+  float y[E];
+  vec_unpack<DT>(raw, y);
+  const bool here = i == (uint32_t)token / E;
+#pragma unroll
+  for (int k = 0; k < E; ++k) {
+    const float x = y[k];
+    float t = (x - c.m) * a.k2;
+    if constexpr (kSlope) t = fmaxf(t, kLeastExponent);
+    const float e = __builtin_amdgcn_exp2f(t);
+    y[k] = e * (kSlope ? __builtin_fmaf(c.p1, t, c.p0) : c.p0);
+    if (here && (uint32_t)token % E == (uint32_t)k && x > kMaskedRow) y[k] += c.at;
+  }
+  return vec_pack<DT>(y);
 }
 
 struct GradArgs {
@@ -154,21 +186,12 @@ __global__ __launch_bounds__(kGradThreads) void espo_logits_grad_kernel(RowArgs 
     if (d.dentropy) h = d.dentropy[row];
   }
   const float2 st = d.stats[row];
-  const float per = 1.0f / (a.temperature * st.y);
-  const float p0 = -(h != 0.0f ? g + h * (d.entropy[row] - logf(st.y)) : g) * per, p1 = -h * kLn2 * per;
+  const RowGrad c = row_grad(a, st.x, st.y, h != 0.0f ? d.entropy[row] : 0.0f, g, h);
 #pragma unroll
   for (int j = 0; j < kGradLoads; ++j) {
     const uint32_t i = base + j * kGradThreads + threadIdx.x;
     if (i >= nvec) break;
-    float y[E];
-    vec_unpack<DT>(r[j], y);
-#pragma unroll
-    for (int k = 0; k < E; ++k) {
-      const float t = fmaxf((y[k] - st.x) * a.k2, kLeastExponent);
-      const float at = i * E + k == (uint32_t)token && y[k] > kMaskedRow ? g / a.temperature : 0.0f;
-      y[k] = y[k] > kMaskedRow ? __builtin_amdgcn_exp2f(t) * (p0 + p1 * t) + at : 0.0f;
-    }
-    vec_store<DT>(out, i, a.V, vec_pack<DT>(y));
+    vec_store<DT>(out, i, a.V, c.p1 != 0.0f ? grad_vec<DT, true>(a, c, r[j], i, token) : grad_vec<DT, false>(a, c, r[j], i, token));
   }
 }
 

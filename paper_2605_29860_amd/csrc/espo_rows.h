@@ -96,6 +96,55 @@ __device__ __forceinline__ void vec_store(char* row, uint32_t i, uint32_t V, u32
   }
 }
 
+// A row of V logits as tiles of 64 vectors, one per lane of a wave.
+struct RowView {
+  const char* x;
+  uint32_t V, nvec, ntiles;
+};
+template <int DT>
+__device__ __forceinline__ RowView row_view(const char* x, uint32_t V) {
+  const uint32_t nvec = (V + vec_elems<DT>() - 1) / vec_elems<DT>();
+  return RowView{x, V, nvec, (nvec + kWave - 1) / kWave};
+}
+
+constexpr int kAhead = 4;  // vectors of a lane in flight
+
+// Calls use(t, raw) for tiles t, t + step, t + 2 step, t + 3 step at a time, starting at `first` and below `end`, while the next four
+// are loaded.  A vector's index is clamped to the row's last one, so that every load is in bounds and none waits for a branch;
+// tile_logits masks what lies beyond V, and `use` leaves out tiles at or beyond `end`.
+template <typename Use>
+__device__ __forceinline__ void stream_tiles(const RowView& r, uint32_t first, uint32_t end, uint32_t step, Use&& use) {
+  const uint32_t lane = threadIdx.x & (kWave - 1);
+  const auto load = [&](uint32_t t) {
+    return __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min(t * kWave + lane, r.nvec - 1) * 16));
+  };
+  if (first >= end) return;
+  u32x4 cur[kAhead], nxt[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) cur[j] = load(first + j * step);
+#pragma unroll 1
+  for (uint32_t t = first; t < end; t += kAhead * step) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) nxt[j] = load(min(t + (kAhead + j) * step, end - 1));
+    use(t, cur);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) cur[j] = nxt[j];
+  }
+}
+
+// The lane's logits of tile t; those at or beyond V are masked.
+template <int DT>
+__device__ __forceinline__ void tile_logits(const RowView& r, uint32_t t, u32x4 raw, float y[vec_elems<DT>()]) {
+  constexpr uint32_t E = vec_elems<DT>();
+  vec_unpack<DT>(raw, y);
+  if (t + 1 >= r.ntiles) {  // the row's last tile
+    const uint32_t i = t * kWave + (threadIdx.x & (kWave - 1));
+#pragma unroll
+    for (uint32_t j = 0; j < E; ++j)
+      if (i * E + j >= r.V) y[j] = kNegInf;
+  }
+}
+
 template <int DT>
 __device__ __forceinline__ float logit_at(const char* row, uint32_t v) {
   if constexpr (DT == ESPO_BF16)

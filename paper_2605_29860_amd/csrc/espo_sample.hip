@@ -45,6 +45,17 @@ __device__ __forceinline__ int bin_of(uint32_t bits) {
   const int j = min(max((int)((bits >> 16) & 0x7fffu) - kMagBelow, 0), kMagSpan + 1), s = (int32_t)bits >> 31;
   return kBinZero + ((j ^ s) - s);
 }
+// The same for the two bf16 numbers in a word, as byte offsets of entries of `kEntry` bytes.
+template <int kEntry>
+__device__ __forceinline__ uint32_t bins_of_pair(uint32_t w) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  typedef short i16x2 __attribute__((ext_vector_type(2)));
+  u16x2 j = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, w & 0x7fff7fffu), (u16x2)(unsigned short)kMagBelow);
+  j = __builtin_elementwise_min(j, (u16x2)(unsigned short)(kMagSpan + 1));
+  const i16x2 s = __builtin_bit_cast(i16x2, w) >> 15;
+  const i16x2 b = (__builtin_bit_cast(i16x2, j) ^ s) - s;
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(u16x2, b) * (unsigned short)kEntry + (u16x2)(unsigned short)(kBinZero * kEntry));
+}
 // The number of a bin: the one nearest to 0 that falls into it.
 __device__ __forceinline__ float bin_number(int bin) {
   const int j = bin - kBinZero;
@@ -119,11 +130,28 @@ struct SampleShared {
 };
 
 // The inclusive sums over the lanes before and at this one.
-template <typename T>
-__device__ __forceinline__ T wave_scan(T v) {
+__device__ __forceinline__ double wave_scan(double v) {
+  v += dpp_f64<kDppRowShr1, 0xf>(v);
+  v += dpp_f64<kDppRowShr2, 0xf>(v);
+  v += dpp_f64<kDppRowShr4, 0xf>(v);
+  v += dpp_f64<kDppRowShr8, 0xf>(v);
+  v += dpp_f64<kDppBcast15, 0xa>(v);
+  v += dpp_f64<kDppBcast31, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += dpp_u32<kDppRowShr1, 0xf>(0u, v);
+  v += dpp_u32<kDppRowShr2, 0xf>(0u, v);
+  v += dpp_u32<kDppRowShr4, 0xf>(0u, v);
+  v += dpp_u32<kDppRowShr8, 0xf>(0u, v);
+  v += dpp_u32<kDppBcast15, 0xa>(0u, v);
+  v += dpp_u32<kDppBcast31, 0xc>(0u, v);
+  return v;
+}
+__device__ __forceinline__ u64 wave_scan(u64 v) {
 #pragma unroll
   for (int d = 1; d < kWave; d *= 2) {
-    const T o = __shfl_up(v, d);
+    const u64 o = __shfl_up(v, d);
     if ((int)(threadIdx.x & (kWave - 1)) >= d) v += o;
   }
   return v;
@@ -198,6 +226,20 @@ __device__ __forceinline__ void logits_of(const Row& r, uint32_t i, u32x4 raw, f
     for (uint32_t j = 0; j < E; ++j)
       if (i * E + j >= r.V) y[j] = kNegInf;
   }
+}
+
+// Logit j of a vector.
+template <int DT>
+__device__ __forceinline__ float logit_in(u32x4 raw, uint32_t j) {
+  const uint32_t q = DT == ESPO_BF16 ? j >> 1 : j;
+  uint32_t w = raw[0];
+#pragma unroll
+  for (uint32_t i = 1; i < 4; ++i) {
+    const uint32_t wi = raw[i];
+    w = q == i ? wi : w;
+  }
+  if constexpr (DT == ESPO_BF16) w = j & 1 ? w & 0xffff0000u : w << 16;
+  return __builtin_bit_cast(float, w);
 }
 
 template <int E>
@@ -314,8 +356,10 @@ template <int DT, typename Kept>
 __device__ __forceinline__ void draw_in_vectors(const SampleArgs& a, int64_t b, const Row& r, uint32_t i, bool mine, double rest, double total,
                                                 Kept&& kept) {
   constexpr uint32_t E = vec_elems<DT>();
+  const u32x4 raw = mine ? vec_load<DT>(r.x, i, r.V) : vec_masked<DT>();
+  const double ln_total = log(total);       // while the load is on its way
   float y[E];
-  vec_unpack<DT>(mine ? vec_load<DT>(r.x, i, r.V) : vec_masked<DT>(), y);
+  vec_unpack<DT>(raw, y);
   double w[E], sum = 0.0;
 #pragma unroll
   for (uint32_t j = 0; j < E; ++j) sum += w[j] = kept(y[j]);
@@ -332,7 +376,7 @@ __device__ __forceinline__ void draw_in_vectors(const SampleArgs& a, int64_t b, 
     upto += w[j];
     found = upto > rest;
   }
-  store_result(a, b, token, (float)(((double)x - r.m) * r.inv_t - log(total)));
+  store_result(a, b, token, (float)(((double)x - r.m) * r.inv_t - ln_total));
 }
 
 // The draw within tiles t0 .. t1 - 1, where the running sum falls: the tiles' sums, the tile, its vectors.
@@ -532,18 +576,33 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
     ESPO_DPP_STEP("v_max_f32", top, "row_shr:8 row_mask:0xf bank_mask:0xf");
     if (lane % kBlockVecs == kBlockVecs - 1) blocks[t * (kWave / kBlockVecs) + lane / kBlockVecs] = top;
     if (counts) {
+      if constexpr (kOne) {
+        float low = y[0], least = fabsf(y[0]);
 #pragma unroll
-      for (uint32_t j = 0; j < E; ++j)
-        if (y[j] > -kBinsBelow) atomicAdd(&count[bin_of(__builtin_bit_cast(uint32_t, y[j]))], 1u);
-      if (kOne && p > 0.0f) {
-        float least = fabsf(y[0]);
+        for (uint32_t j = 1; j < E; ++j) low = fminf(low, y[j]), least = fminf(least, fabsf(y[j]));
+        const bool all = __builtin_amdgcn_ballot_w64(!(low > -kBinsBelow)) == 0;
 #pragma unroll
-        for (uint32_t j = 1; j < E; ++j) least = fminf(least, fabsf(y[j]));
-        if (least < 0x1p-10f) {
-#pragma unroll
-          for (uint32_t j = 0; j < E; ++j)
-            if (fabsf(y[j]) < 0x1p-10f) next_to_0 += exp2_f64((double)y[j] * r.c);
+        for (uint32_t j = 0; j < 4; ++j) {
+          const uint32_t at = bins_of_pair<4>(raw[j]);
+          if (all) {
+            atomicAdd((uint32_t*)(lds + (at & 0xffffu)), 1u);
+            atomicAdd((uint32_t*)(lds + (at >> 16)), 1u);
+          } else {                          // masked logits would all wait for one counter
+            if (y[2 * j] > -kBinsBelow) atomicAdd((uint32_t*)(lds + (at & 0xffffu)), 1u);
+            if (y[2 * j + 1] > -kBinsBelow) atomicAdd((uint32_t*)(lds + (at >> 16)), 1u);
+          }
         }
+        if (p > 0.0f && __builtin_amdgcn_ballot_w64(least < 0x1p-10f) != 0) {
+#pragma unroll 1
+          for (uint32_t j = 0; j < E; ++j) {
+            const float v = logit_in<DT>(raw, j);
+            if (fabsf(v) < 0x1p-10f) next_to_0 += exp2_f64((double)v * r.c);
+          }
+        }
+      } else {
+#pragma unroll
+        for (uint32_t j = 0; j < E; ++j)
+          if (y[j] > -kBinsBelow) atomicAdd(&count[bin_of(__builtin_bit_cast(uint32_t, y[j]))], 1u);
       }
     }
     if (masses) {
@@ -595,8 +654,7 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
       }
       __syncthreads();
       kbin = (int)s.found_bin;
-      if constexpr (kOne) {
-        known = kbin != kBinZero;
+      if (kOne && kbin != kBinZero) {
         cut = bin_number(kbin);
       } else {
         const uint32_t rank = (uint32_t)k - s.above_count;  // within the bin, from 1
@@ -626,40 +684,37 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
       zero *= exp2_f64(-r.m * r.c);
       __syncthreads();
     }
-    const auto bin_mass = [&](int bin) {
-      if (bin <= 0 || bin < kbin) return 0.0;
-      if constexpr (kOne) {
-        if (bin == kBinZero) return zero;
-        const uint32_t c = count[bin];
-        return c ? (double)c * r.weight(bin_number(bin)) : 0.0;
-      } else {
-        if (bin == kbin && k > 0) return (double)s.kept_mass * (1.0 / kFixed);
-        const u64 w = mass[bin];
-        return w ? (double)w * (1.0 / kBinMass) * r.weight(bin_number(bin)) : 0.0;
-      }
-    };
-    double mine = 0.0, all;
-#pragma unroll 1
-    for (int i = 0; i < kEach; ++i) mine += bin_mass(highest - i);
+    const bool ranked = k > 0 && !(kOne && kbin != kBinZero);  // bin kbin has been ranked for top-k
+    double w[kEach], mine = 0.0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int bin = highest - i;
+      double n = 0.0;
+      if (bin > 0) n = kOne ? (double)count[bin] : (double)mass[bin] * (1.0 / kBinMass);
+      w[i] = n * r.weight(bin_number(bin));
+      if (kOne && bin == kBinZero) w[i] = zero;
+      if (bin < kbin) w[i] = 0.0;
+      if (ranked && bin == kbin) w[i] = (double)s.kept_mass * (1.0 / kFixed);
+      mine += w[i];
+    }
     double before = block_before<W>(mine, s.wave_f64, all);
     const double target = (double)p * all;
     const uint32_t who = block_pick<W>(before, mine, kNoWeight, target, true, s);
     if (threadIdx.x == who) {
-#pragma unroll 1
+      bool done = false;
+#pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const double w = bin_mass(highest - i);
-        if (!(w > kNoWeight)) continue;
+        if (done || !(w[i] > kNoWeight)) continue;
         s.found_bin = (uint32_t)(highest - i);
         s.rest = before;
-        before += w;
-        if (before >= target) break;
+        before += w[i];
+        done = before >= target;
       }
     }
     __syncthreads();
     const int bin = (int)s.found_bin;
     const double above = s.rest;
-    if constexpr (kOne) {
-      known = bin != kBinZero;
+    if (kOne && bin != kBinZero) {
       cut = bin_number(bin);
     } else {
       if (bin != kbin || k == 0) known = collect_members<DT, W>(r, bin, blocks, nblocks, members, s);
@@ -729,9 +784,11 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
         if (q >= nvisit) break;
         float y[E];
         logits_of<DT>(r, visit[q] * kBlockVecs + sub, cur[h], y);
-        double w = 0.0;
+        uint32_t in = 0;                    // most vectors hold one kept logit or none
 #pragma unroll
-        for (uint32_t e = 0; e < E; ++e) w += kept(y[e]);
+        for (uint32_t e = 0; e < E; ++e) in |= y[e] >= cut && y[e] > kMaskedRow ? 1u << e : 0u;
+        double w = 0.0;
+        for (; in != 0; in &= in - 1) w += kept(logit_in<DT>(cur[h], (uint32_t)__builtin_ctz(in)));
         w += dpp_f64<kDppRowShr1, 0xf>(w);
         w += dpp_f64<kDppRowShr2, 0xf>(w);
         w += dpp_f64<kDppRowShr4, 0xf>(w);
@@ -809,7 +866,7 @@ size_t filter_lds(int64_t V, uint32_t& blocks, uint32_t& members) {
   first = (first + 15) / 16 * 16;
   blocks = (uint32_t)first;
   members = (uint32_t)(first + (nblocks + 3) / 4 * 16);
-  return members + (DT == ESPO_BF16 ? 0 : (size_t)kMostMembers * 4);
+  return members + (size_t)kMostMembers * 4;
 }
 
 template <int DT, int W>
