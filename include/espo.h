@@ -528,8 +528,9 @@ size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
  * t_v = (x_v - max x) / temperature, S = sum_v exp t_v and pi_v = exp(t_v) / S:
  *   logprob[n] = t_a - ln S for a = tokens[n],       entropy[n] = ln S - sum_v pi_v t_v,
  *   dlogits[n,v] = (g ([v = a] - pi_v) - h pi_v (ln pi_v + entropy[n])) / temperature
- * where g = dlogprob[n] and h = dentropy[n] are the loss's derivatives.  The sums are fp32; a gradient is rounded to the
- * logits' type once, as it is stored.
+ * where g = dlogprob[n] and h = dentropy[n] are the loss's derivatives.  The sums are fp32, in an order that
+ * follows the launch layout (which depends on N, V, the type and what is asked for, and on nothing else); a gradient is rounded to
+ * the logits' type once, as it is stored.
  * A row whose token is outside [0, V) is not used (padding, a prompt): its logits are not read, logprob and entropy
  * are 0 and its gradient is 0.  Masked logits (at or below -1e30) have probability and gradient 0; a token that is
  * masked itself has logprob -inf.  NaN and +inf are not supported in rows that are used (results for that row are

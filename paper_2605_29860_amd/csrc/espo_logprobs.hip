@@ -20,6 +20,8 @@ namespace {
 constexpr int kRowWaves = 8, kRowThreads = kRowWaves * kWave;
 constexpr int kGradThreads = 256, kGradLoads = 4;
 constexpr int kGradSpan = kGradThreads * kGradLoads;  // vectors of a workgroup
+constexpr int kComputeUnits = 256;
+constexpr int64_t kHeldRows = 192;               // fewer rows leave compute units idle where one workgroup holds a row
 constexpr int kSumThreads = 1024, kSumWaves = kSumThreads / kWave;
 
 struct RowArgs {
@@ -195,6 +197,101 @@ __global__ __launch_bounds__(kGradThreads) void espo_logits_grad_kernel(RowArgs 
   }
 }
 
+// Forward, objective and gradient of a row by one workgroup that holds the row in registers, so that the logits come in once and the gradient
+// goes out once.  A workgroup takes rows blockIdx.x, blockIdx.x + gridDim.x, ...; as a vector's gradient is stored, its registers take the
+// same vector of the next row, so that loads and stores are under way while the exponentials of both passes are formed.
+constexpr int kHeld = 20;                        // vectors of a thread: 80 of the 128 registers that 16 waves per compute unit leave
+
+// Keeps what was formed from a vector before from being kept in registers of its own (its logits as floats take twice the room).
+__device__ __forceinline__ void hold(u32x4& v) { asm volatile("" : "+v"(v)); }
+
+template <int DT, int W, bool kSlope>
+__global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))) void espo_policy_kernel(RowArgs a, RowOutputs o, GradArgs d, PolicyArgs q) {
+  __shared__ SoftmaxSums lds[2][W];
+  constexpr uint32_t E = vec_elems<DT>(), kThreads = W * kWave;
+  const uint32_t nvec = (a.V + E - 1) / E;
+  const int last = (int)((nvec - 1) / kThreads);  // of the vectors raw[0 .. last] of a thread, all but the last lie within the row
+  const uint32_t last_vec = last * kThreads + threadIdx.x;
+  // Vector r of a row; of a row that is not used the same one again and again, so that no register waits for a branch.
+  const auto load = [&](const char* x, bool used, int r) {
+    return __builtin_nontemporal_load((const u32x4*)(x + (size_t)min((used ? r * kThreads : 0) + threadIdx.x, nvec - 1) * 16));
+  };
+  int64_t row = blockIdx.x;
+  int32_t token = a.tokens[row];
+  const char* x = a.logits + row * a.row_bytes;
+  u32x4 raw[kHeld];
+#pragma unroll
+  for (int r = 0; r < kHeld; ++r) raw[r] = load(x, used_row(token, a.V), r);
+  for (int turn = 0;; turn ^= 1) {
+    const bool used = used_row(token, a.V), more = row + gridDim.x < a.N;
+    const int64_t next = more ? row + gridDim.x : row;
+    const int32_t next_token = more ? a.tokens[next] : -1;
+    const bool next_used = used_row(next_token, a.V);
+    const char* next_x = a.logits + next * a.row_bytes;
+    char* out = d.dlogits + row * d.grad_bytes;
+    RowGrad g;
+    u32x4 tail = vec_masked<DT>();
+    if (used) {
+      const float x_token = logit_at<DT>(x, (uint32_t)token), adv = q.adv[row];
+      SoftmaxSums p{kMaskedRow, 0.0f, 0.0f};
+#pragma unroll
+      for (int r = 0; r < kHeld; ++r) {
+        if (r < last) {
+          float y[E], m = p.m;
+          hold(raw[r]);
+          vec_unpack<DT>(raw[r], y);
+#pragma unroll
+          for (uint32_t k = 0; k < E; ++k) m = fmaxf(m, y[k]);
+          rescale<true>(p, m, a.k2);
+#pragma unroll
+          for (uint32_t k = 0; k < E; ++k) add_logit<true>(p, y[k], a.k2);
+        } else if (r == last) {
+          tail = raw[r];
+        }
+      }
+      {
+        float y[E], m = p.m;
+        vec_unpack<DT>(tail, y);
+#pragma unroll
+        for (uint32_t k = 0; k < E; ++k) {
+          if (last_vec * E + k >= a.V) y[k] = kNegInf;
+          m = fmaxf(m, y[k]);
+        }
+        rescale<true>(p, m, a.k2);
+#pragma unroll
+        for (uint32_t k = 0; k < E; ++k) add_logit<true>(p, y[k], a.k2);
+      }
+      p = block_merge<W, true>(p, a.k2, lds[turn]);
+      float logprob, entropy;
+      float2 stats;
+      row_results(a, x_token, p, logprob, entropy, stats);
+      if (threadIdx.x == 0) store_row(o, row, logprob, entropy, stats);
+      const Surrogate c = surrogate(q, row, logprob, adv);
+      g = row_grad(a, stats.x, stats.y, entropy, c.cut ? 0.0f : -c.weight * c.ratio * adv, kSlope ? -c.weight * q.entropy_coef : 0.0f);
+    } else if (threadIdx.x == 0) {
+      store_row(o, row, 0.0f, 0.0f, float2{0.0f, 1.0f});
+    }
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+      hold(raw[r]);
+      if (r < last) {
+        const uint32_t i = r * kThreads + threadIdx.x;
+        u32x4 v{0, 0, 0, 0};
+        if (used) v = grad_vec<DT, kSlope>(a, g, raw[r], i, token);
+        __builtin_nontemporal_store(v, (u32x4*)(out + (size_t)i * 16));
+      }
+      raw[r] = load(next_x, next_used, r);
+    }
+    if (last_vec < nvec) {
+      u32x4 v{0, 0, 0, 0};
+      if (used) v = grad_vec<DT, kSlope>(a, g, tail, last_vec, token);
+      vec_store<DT>(out, last_vec, a.V, v);
+    }
+    if (!more) return;
+    row = next, token = next_token, x = next_x;
+  }
+}
+
 // The sums of the objective over all rows, in double and in a fixed order: one workgroup, thread i takes rows i, i + 1024, ...
 __global__ __launch_bounds__(kSumThreads) void espo_policy_sums_kernel(const int32_t* tokens, const float* logprob, const float* entropy,
                                                                        int64_t N, uint32_t V, PolicyArgs q, espo_policy_result* out) {
@@ -245,6 +342,38 @@ void backward(const RowArgs& a, const GradArgs& d, const PolicyArgs& q, hipStrea
   hipLaunchKernelGGL((espo_logits_grad_kernel<DT, kPolicy>), dim3((unsigned)(a.N * d.spans)), dim3(kGradThreads), 0, stream, a, d, q);
 }
 
+// Waves of the workgroup that holds a row of V logits, 0 if none does.
+template <int DT>
+int held_waves(int64_t V) {
+  const int64_t nvec = (V + vec_elems<DT>() - 1) / vec_elems<DT>();
+  for (int w = 4; w <= 16; w *= 2)
+    if (nvec <= (int64_t)w * kWave * kHeld) return w;
+  return 0;
+}
+
+template <int DT, int W>
+void policy_held(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, hipStream_t stream) {
+  const int64_t groups = kComputeUnits * (16 / W);
+  const dim3 grid((unsigned)(a.N < groups ? a.N : groups)), block(W * kWave);
+  if (q.entropy_coef != 0.0f)
+    hipLaunchKernelGGL((espo_policy_kernel<DT, W, true>), grid, block, 0, stream, a, o, d, q);
+  else
+    hipLaunchKernelGGL((espo_policy_kernel<DT, W, false>), grid, block, 0, stream, a, o, d, q);
+}
+
+// Log-probabilities, entropy and, if it is wanted, the gradient of the objective.
+template <int DT>
+void policy(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, hipStream_t stream) {
+  const int waves = d.dlogits && a.N >= kHeldRows ? held_waves<DT>(a.V) : 0;
+  switch (waves) {
+    case 4: return policy_held<DT, 4>(a, o, d, q, stream);
+    case 8: return policy_held<DT, 8>(a, o, d, q, stream);
+    case 16: return policy_held<DT, 16>(a, o, d, q, stream);
+  }
+  forward<DT>(a, o, stream);
+  if (d.dlogits) backward<DT, true>(a, d, q, stream);
+}
+
 uint32_t grad_spans(int dt, int64_t V) {
   const int64_t span = (int64_t)kGradSpan * (dt == ESPO_BF16 ? 8 : 4);
   return (uint32_t)((V + span - 1) / span);
@@ -289,14 +418,9 @@ int launch_policy_loss(const void* logits, int dt, int64_t N, int64_t V, int64_t
   const RowOutputs o{logprob, entropy, stats};
   const GradArgs d{(char*)dlogits, grad_stride * (dt == ESPO_BF16 ? 2 : 4), grad_spans(dt, V), stats, entropy, nullptr, nullptr, logprob};
   if (N > 0) {
-    if (dt == ESPO_BF16) forward<ESPO_BF16>(a, o, stream);
-    else forward<ESPO_F32>(a, o, stream);
+    if (dt == ESPO_BF16) policy<ESPO_BF16>(a, o, d, q, stream);
+    else policy<ESPO_F32>(a, o, d, q, stream);
     if (launched() != ESPO_OK) return ESPO_EHIP;
-    if (dlogits) {
-      if (dt == ESPO_BF16) backward<ESPO_BF16, true>(a, d, q, stream);
-      else backward<ESPO_F32, true>(a, d, q, stream);
-      if (launched() != ESPO_OK) return ESPO_EHIP;
-    }
   }
   hipLaunchKernelGGL(espo_policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, stream, tokens, logprob, entropy, N, (uint32_t)V, q, out);
   return launched();

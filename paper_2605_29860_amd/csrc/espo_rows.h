@@ -88,7 +88,9 @@ __device__ __forceinline__ void vec_store(char* row, uint32_t i, uint32_t V, u32
     __builtin_nontemporal_store(r, (u32x4*)(row + (size_t)i * 16));
     return;
   }
-  for (uint32_t j = 0; i * E + j < V; ++j) {
+#pragma unroll
+  for (uint32_t j = 0; j < E; ++j) {
+    if (i * E + j >= V) break;
     if constexpr (DT == ESPO_BF16)
       ((uint16_t*)row)[i * E + j] = (uint16_t)(r[j >> 1] >> (16 * (j & 1)));
     else
