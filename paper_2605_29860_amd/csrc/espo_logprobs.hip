@@ -28,7 +28,7 @@ struct RowArgs {
   const char* logits;
   int64_t row_bytes, N;
   uint32_t V;
-  float temperature, k2;
+  float temperature, inv_t, k2;
   const int32_t* tokens;
 };
 
@@ -43,8 +43,8 @@ __device__ __forceinline__ bool used_row(int32_t token, uint32_t V) { return (ui
 __device__ __forceinline__ void row_results(const RowArgs& a, float x_token, const SoftmaxSums& p, float& logprob, float& entropy, float2& stats) {
   const bool any = p.m > kMaskedRow;
   const float ln_s = any ? logf(p.s) : 0.0f;
-  logprob = x_token > kMaskedRow ? -(p.m - x_token) / a.temperature - ln_s : kNegInf;
-  entropy = any ? ln_s - p.a / p.s * kLn2 : 0.0f;
+  logprob = x_token > kMaskedRow ? -(p.m - x_token) * a.inv_t - ln_s : kNegInf;
+  entropy = any ? ln_s - p.a * __builtin_amdgcn_rcpf(p.s) * kLn2 : 0.0f;
   stats = any ? float2{p.m, p.s} : float2{0.0f, 1.0f};
 }
 
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kRowThreads) void espo_logprobs_kernel(RowArgs a, R
 #pragma unroll
       for (int i = 0; i < E; ++i) m = fmaxf(m, y[j][i]);
     }
-    rescale<kEntropy>(p, m, a.k2);
+    follow<kEntropy>(p, m, a.k2);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
       if (t + j * kRowWaves < r.ntiles) {
@@ -105,17 +105,23 @@ struct PolicyArgs {
 };
 
 struct Surrogate {
-  float ratio, diff, weight;
+  float ratio, diff;
   bool cut;  // the clipped branch is the smaller one, and no gradient passes
 };
 
+struct TokenInputs {
+  float old_logprob, adv, weight;
+};
+__device__ __forceinline__ TokenInputs token_inputs(const PolicyArgs& q, int64_t row) {
+  return TokenInputs{q.old_logprob[row], q.adv[row], q.scale * (q.weights ? q.weights[row] : 1.0f)};
+}
+
 // The ratio is held below e^88, the largest power of e that fp32 holds: a product with an advantage of 0 stays 0.
-__device__ __forceinline__ Surrogate surrogate(const PolicyArgs& q, int64_t row, float logprob, float adv) {
+__device__ __forceinline__ Surrogate surrogate(const PolicyArgs& q, const TokenInputs& in, float logprob) {
   Surrogate c;
-  c.diff = logprob - q.old_logprob[row];
+  c.diff = logprob - in.old_logprob;
   c.ratio = expf(fminf(c.diff, 88.0f));
-  c.weight = q.scale * (q.weights ? q.weights[row] : 1.0f);
-  c.cut = adv >= 0.0f ? c.ratio > 1.0f + q.clip_high : c.ratio < 1.0f - q.clip_low;
+  c.cut = in.adv >= 0.0f ? c.ratio > 1.0f + q.clip_high : c.ratio < 1.0f - q.clip_low;
   return c;
 }
 
@@ -126,8 +132,8 @@ struct RowGrad {
 
 // m, s: the row's largest logit and sum; `entropy` only counts where h is not 0.
 __device__ __forceinline__ RowGrad row_grad(const RowArgs& a, float m, float s, float entropy, float g, float h) {
-  const float per = 1.0f / (a.temperature * s);
-  return RowGrad{m, -(h != 0.0f ? g + h * (entropy - logf(s)) : g) * per, -h * kLn2 * per, g / a.temperature};
+  const float per = a.inv_t * __builtin_amdgcn_rcpf(s);
+  return RowGrad{m, -(h != 0.0f ? g + h * (entropy - logf(s)) : g) * per, -h * kLn2 * per, g * a.inv_t};
 }
 
 template <int DT, bool kSlope>
@@ -179,10 +185,10 @@ __global__ __launch_bounds__(kGradThreads) void espo_logits_grad_kernel(RowArgs 
   for (int j = 0; j < kGradLoads; ++j) r[j] = vec_load<DT>(x, base + j * kGradThreads + threadIdx.x, a.V);
   float g, h = 0.0f;
   if constexpr (kPolicy) {
-    const float adv = q.adv[row];
-    const Surrogate c = surrogate(q, row, d.logprob[row], adv);
-    g = c.cut ? 0.0f : -c.weight * c.ratio * adv;
-    h = -c.weight * q.entropy_coef;
+    const TokenInputs in = token_inputs(q, row);
+    const Surrogate c = surrogate(q, in, d.logprob[row]);
+    g = c.cut ? 0.0f : -in.weight * c.ratio * in.adv;
+    h = -in.weight * q.entropy_coef;
   } else {
     g = d.dlogprob[row];
     if (d.dentropy) h = d.dentropy[row];
@@ -198,97 +204,148 @@ __global__ __launch_bounds__(kGradThreads) void espo_logits_grad_kernel(RowArgs 
 }
 
 // Forward, objective and gradient of a row by one workgroup that holds the row in registers, so that the logits come in once and the gradient
-// goes out once.  A workgroup takes rows blockIdx.x, blockIdx.x + gridDim.x, ...; as a vector's gradient is stored, its registers take the
-// same vector of the next row, so that loads and stores are under way while the exponentials of both passes are formed.
+// goes out once.  While a row's sums are formed, the first vectors of the workgroup's next row travel to LDS; as a vector's gradient is
+// stored, its registers take that vector of the next row, from LDS or from memory.  So there is always something under way, also
+// where all compute units are at the same point, which they are more often than not.  The workgroups share the used rows
+// evenly, by rank among the used rows, and then the zeros of the unused ones, from the other end.
 constexpr int kHeld = 20;                        // vectors of a thread: 80 of the 128 registers that 16 waves per compute unit leave
+constexpr int kStaged = 8;                       // of them through LDS: 128 KB of the compute unit's 160
+constexpr int kDealt = 1024;                     // rows of a workgroup
+constexpr int64_t kDealtEach = kDealt - 2;       // of both kinds together, rounded up each
 
 // Keeps what was formed from a vector before from being kept in registers of its own (its logits as floats take twice the room).
 __device__ __forceinline__ void hold(u32x4& v) { asm volatile("" : "+v"(v)); }
 
+// The workgroup's share of the rows: the used ones from the front of `rows`, the others from its end, and how many of each.
+template <int W>
+__device__ __forceinline__ void deal_rows(const RowArgs& a, int32_t* rows, uint32_t (*counts)[W], int& nused, int& nother) {
+  const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, groups = gridDim.x, g = blockIdx.x, N = (uint32_t)a.N;
+  uint32_t base = 0;                             // used rows so far
+#pragma unroll 1
+  for (uint32_t row = 0; row < N; row += W * kWave) {
+    const bool mine = row + threadIdx.x < N, used = mine && used_row(a.tokens[row + threadIdx.x], a.V);
+    const uint64_t mask = __builtin_amdgcn_ballot_w64(used);
+    uint32_t* count = counts[(row / (W * kWave)) & 1];
+    if (lane == 0) count[wave] = (uint32_t)__builtin_popcountll(mask);
+    __syncthreads();
+    uint32_t rank = base + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+#pragma unroll
+    for (uint32_t w = 0; w < W; ++w) {
+      rank += w < wave ? count[w] : 0;
+      base += count[w];
+    }
+    const uint32_t other = row + threadIdx.x - rank;
+    if (used) {
+      if (rank % groups == g) rows[rank / groups] = (int32_t)(row + threadIdx.x);
+    } else if (mine) {
+      if (other % groups == groups - 1 - g) rows[kDealt - 1 - other / groups] = (int32_t)(row + threadIdx.x);
+    }
+  }
+  __syncthreads();
+  const uint32_t others = N - base, h = groups - 1 - g;
+  nused = (int)(base > g ? (base - g + groups - 1) / groups : 0);
+  nother = (int)(others > h ? (others - h + groups - 1) / groups : 0);
+}
+
 template <int DT, int W, bool kSlope>
 __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))) void espo_policy_kernel(RowArgs a, RowOutputs o, GradArgs d, PolicyArgs q) {
-  __shared__ SoftmaxSums lds[2][W];
   constexpr uint32_t E = vec_elems<DT>(), kThreads = W * kWave;
+  extern __shared__ __align__(16) u32x4 staged[];  // [kStaged][kThreads]
+  __shared__ SoftmaxSums lds[2][W];
+  __shared__ uint32_t counts[2][W];
+  __shared__ int32_t rows[kDealt];
   const uint32_t nvec = (a.V + E - 1) / E;
   const int last = (int)((nvec - 1) / kThreads);  // of the vectors raw[0 .. last] of a thread, all but the last lie within the row
-  const uint32_t last_vec = last * kThreads + threadIdx.x;
-  // Vector r of a row; of a row that is not used the same one again and again, so that no register waits for a branch.
-  const auto load = [&](const char* x, bool used, int r) {
-    return __builtin_nontemporal_load((const u32x4*)(x + (size_t)min((used ? r * kThreads : 0) + threadIdx.x, nvec - 1) * 16));
+  // The thread's index, not to be seen through: its vectors' offsets would be kept in registers from row to row.
+  const auto own_index = [] {
+    uint32_t t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
   };
-  int64_t row = blockIdx.x;
-  int32_t token = a.tokens[row];
-  const char* x = a.logits + row * a.row_bytes;
+  // Where vector r of a row is, or where there is no row to come the same one again and again: no register waits for a branch.  (Those behind
+  // the row's last vector are that one.)
+  const auto place = [&](const char* x, bool any, int r) { return x + (size_t)min((any ? r * kThreads : 0) + own_index(), nvec - 1) * 16; };
+  int nused, nother;
+  deal_rows<W>(a, rows, counts, nused, nother);
+  const auto row_at = [&](int i) { return (int64_t)__builtin_amdgcn_readfirstlane(rows[i]); };
   u32x4 raw[kHeld];
+  {
+    const char* x = a.logits + (nused > 0 ? row_at(0) : 0) * a.row_bytes;
 #pragma unroll
-  for (int r = 0; r < kHeld; ++r) raw[r] = load(x, used_row(token, a.V), r);
-  for (int turn = 0;; turn ^= 1) {
-    const bool used = used_row(token, a.V), more = row + gridDim.x < a.N;
-    const int64_t next = more ? row + gridDim.x : row;
-    const int32_t next_token = more ? a.tokens[next] : -1;
-    const bool next_used = used_row(next_token, a.V);
-    const char* next_x = a.logits + next * a.row_bytes;
+    for (int r = 0; r < kHeld; ++r) raw[r] = __builtin_nontemporal_load((const u32x4*)place(x, nused > 0, r));
+  }
+#pragma unroll 1
+  for (int i = 0; i < nused; ++i) {
+    const int64_t row = row_at(i);
+    const bool more = i + 1 < nused;
+    const char* x = a.logits + row * a.row_bytes;
+    const char* next_x = a.logits + row_at(more ? i + 1 : i) * a.row_bytes;
     char* out = d.dlogits + row * d.grad_bytes;
-    RowGrad g;
+    const int32_t token = a.tokens[row];
+    const float x_token = logit_at<DT>(x, (uint32_t)token);
+    const TokenInputs in = token_inputs(q, row);
+    __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): what the wave has read from `staged` has arrived
+#pragma unroll
+    for (int r = 0; r < kStaged; ++r)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)place(next_x, more, r),
+                                       (__attribute__((address_space(3))) void*)(staged + r * kThreads + (threadIdx.x & ~63u)), 16, 0, 0);
+    SoftmaxSums p{kMaskedRow, 0.0f, 0.0f};
     u32x4 tail = vec_masked<DT>();
-    if (used) {
-      const float x_token = logit_at<DT>(x, (uint32_t)token), adv = q.adv[row];
-      SoftmaxSums p{kMaskedRow, 0.0f, 0.0f};
 #pragma unroll
-      for (int r = 0; r < kHeld; ++r) {
-        if (r < last) {
-          float y[E], m = p.m;
-          hold(raw[r]);
-          vec_unpack<DT>(raw[r], y);
-#pragma unroll
-          for (uint32_t k = 0; k < E; ++k) m = fmaxf(m, y[k]);
-          rescale<true>(p, m, a.k2);
-#pragma unroll
-          for (uint32_t k = 0; k < E; ++k) add_logit<true>(p, y[k], a.k2);
-        } else if (r == last) {
-          tail = raw[r];
-        }
-      }
-      {
+    for (int r = 0; r < kHeld; ++r) {
+      if (r < last) {
         float y[E], m = p.m;
-        vec_unpack<DT>(tail, y);
+        hold(raw[r]);
+        vec_unpack<DT>(raw[r], y);
 #pragma unroll
-        for (uint32_t k = 0; k < E; ++k) {
-          if (last_vec * E + k >= a.V) y[k] = kNegInf;
-          m = fmaxf(m, y[k]);
-        }
-        rescale<true>(p, m, a.k2);
+        for (uint32_t k = 0; k < E; ++k) m = fmaxf(m, y[k]);
+        follow<true>(p, m, a.k2);
 #pragma unroll
         for (uint32_t k = 0; k < E; ++k) add_logit<true>(p, y[k], a.k2);
+      } else if (r == last) {
+        tail = raw[r];
       }
-      p = block_merge<W, true>(p, a.k2, lds[turn]);
-      float logprob, entropy;
-      float2 stats;
-      row_results(a, x_token, p, logprob, entropy, stats);
-      if (threadIdx.x == 0) store_row(o, row, logprob, entropy, stats);
-      const Surrogate c = surrogate(q, row, logprob, adv);
-      g = row_grad(a, stats.x, stats.y, entropy, c.cut ? 0.0f : -c.weight * c.ratio * adv, kSlope ? -c.weight * q.entropy_coef : 0.0f);
-    } else if (threadIdx.x == 0) {
-      store_row(o, row, 0.0f, 0.0f, float2{0.0f, 1.0f});
     }
+    const uint32_t last_vec = last * kThreads + own_index();
+    {
+      float y[E], m = p.m;
+      vec_unpack<DT>(tail, y);
+#pragma unroll
+      for (uint32_t k = 0; k < E; ++k) {
+        if (last_vec * E + k >= a.V) y[k] = kNegInf;
+        m = fmaxf(m, y[k]);
+      }
+      follow<true>(p, m, a.k2);
+#pragma unroll
+      for (uint32_t k = 0; k < E; ++k) add_logit<true>(p, y[k], a.k2);
+    }
+    p = block_merge<W, true>(p, a.k2, lds[i & 1]);
+    float logprob, entropy;
+    float2 stats;
+    row_results(a, x_token, p, logprob, entropy, stats);
+    if (threadIdx.x == 0) store_row(o, row, logprob, entropy, stats);
+    const Surrogate c = surrogate(q, in, logprob);
+    const RowGrad g = row_grad(a, stats.x, stats.y, entropy, c.cut ? 0.0f : -in.weight * c.ratio * in.adv, kSlope ? -in.weight * q.entropy_coef : 0.0f);
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): the wave's part of `staged` is there
 #pragma unroll
     for (int r = 0; r < kHeld; ++r) {
       hold(raw[r]);
       if (r < last) {
-        const uint32_t i = r * kThreads + threadIdx.x;
-        u32x4 v{0, 0, 0, 0};
-        if (used) v = grad_vec<DT, kSlope>(a, g, raw[r], i, token);
-        __builtin_nontemporal_store(v, (u32x4*)(out + (size_t)i * 16));
+        const uint32_t at = r * kThreads + own_index();
+        __builtin_nontemporal_store(grad_vec<DT, kSlope>(a, g, raw[r], at, token), (u32x4*)(out + (size_t)at * 16));
       }
-      raw[r] = load(next_x, next_used, r);
+      raw[r] = r < kStaged ? staged[r * kThreads + own_index()] : __builtin_nontemporal_load((const u32x4*)place(next_x, more, r));
     }
-    if (last_vec < nvec) {
-      u32x4 v{0, 0, 0, 0};
-      if (used) v = grad_vec<DT, kSlope>(a, g, tail, last_vec, token);
-      vec_store<DT>(out, last_vec, a.V, v);
-    }
-    if (!more) return;
-    row = next, token = next_token, x = next_x;
+    if (last_vec < nvec) vec_store<DT>(out, last_vec, a.V, grad_vec<DT, kSlope>(a, g, tail, last_vec, token));
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);            // the last loads, of no row
+#pragma unroll 1
+  for (int i = 0; i < nother; ++i) {
+    const int64_t row = row_at(kDealt - 1 - i);
+    char* out = d.dlogits + row * d.grad_bytes;
+    if (threadIdx.x == 0) store_row(o, row, 0.0f, 0.0f, float2{0.0f, 1.0f});
+#pragma unroll 1
+    for (uint32_t j = threadIdx.x; j < nvec; j += kThreads) vec_store<DT>(out, j, a.V, u32x4{0, 0, 0, 0});
   }
 }
 
@@ -300,11 +357,11 @@ __global__ __launch_bounds__(kSumThreads) void espo_policy_sums_kernel(const int
   double v[kSums + 1] = {};
   for (int64_t row = threadIdx.x; row < N; row += kSumThreads) {
     if (!used_row(tokens[row], V)) continue;
-    const float adv = q.adv[row];
-    const Surrogate c = surrogate(q, row, logprob[row], adv);
-    const double w = c.weight, H = entropy[row], bound = c.cut ? (adv >= 0.0f ? 1.0 + q.clip_high : 1.0 - q.clip_low) : (double)c.ratio;
-    v[0] += w * (-bound * adv - q.entropy_coef * H);
-    v[1] += w * (-bound * adv);
+    const TokenInputs in = token_inputs(q, row);
+    const Surrogate c = surrogate(q, in, logprob[row]);
+    const double w = in.weight, H = entropy[row], bound = c.cut ? (in.adv >= 0.0f ? 1.0 + q.clip_high : 1.0 - q.clip_low) : (double)c.ratio;
+    v[0] += w * (-bound * in.adv - q.entropy_coef * H);
+    v[1] += w * (-bound * in.adv);
     v[2] += w * H;
     v[3] += w * (exp((double)fminf(c.diff, 88.0f)) - 1.0 - c.diff);
     v[4] += c.cut ? w : 0.0;
@@ -326,7 +383,8 @@ __global__ __launch_bounds__(kSumThreads) void espo_policy_sums_kernel(const int
 
 RowArgs row_args(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens) {
   const int es = dt == ESPO_BF16 ? 2 : 4;
-  return RowArgs{(const char*)logits, row_stride * es, N, (uint32_t)V, temperature, (float)(1.4426950408889634 / (double)temperature), tokens};
+  return RowArgs{(const char*)logits, row_stride * es, N, (uint32_t)V, temperature, 1.0f / temperature,
+                 (float)(1.4426950408889634 / (double)temperature), tokens};
 }
 
 template <int DT>
@@ -351,14 +409,32 @@ int held_waves(int64_t V) {
   return 0;
 }
 
+// The same arguments from row `from` on, for n rows.
+RowArgs rows_from(RowArgs a, int64_t from, int64_t n) {
+  a.logits += from * a.row_bytes;
+  a.tokens += from;
+  a.N = n;
+  return a;
+}
+
 template <int DT, int W>
 void policy_held(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, hipStream_t stream) {
-  const int64_t groups = kComputeUnits * (16 / W);
-  const dim3 grid((unsigned)(a.N < groups ? a.N : groups)), block(W * kWave);
-  if (q.entropy_coef != 0.0f)
-    hipLaunchKernelGGL((espo_policy_kernel<DT, W, true>), grid, block, 0, stream, a, o, d, q);
-  else
-    hipLaunchKernelGGL((espo_policy_kernel<DT, W, false>), grid, block, 0, stream, a, o, d, q);
+  const int64_t groups = a.N < kComputeUnits * (16 / W) ? a.N : kComputeUnits * (16 / W);
+  for (int64_t from = 0; from < a.N; from += groups * kDealtEach) {  // one launch up to 261632 rows
+    const int64_t n = a.N - from < groups * kDealtEach ? a.N - from : groups * kDealtEach;
+    const RowArgs ra = rows_from(a, from, n);
+    const RowOutputs ro{o.logprob + from, o.entropy + from, o.stats + from};
+    GradArgs rd = d;
+    rd.dlogits += from * d.grad_bytes;
+    PolicyArgs rq = q;
+    rq.old_logprob += from, rq.adv += from, rq.weights += q.weights ? from : 0;
+    const dim3 grid((unsigned)(n < groups ? n : groups)), block(W * kWave);
+    const size_t lds = (size_t)kStaged * W * kWave * 16;
+    if (q.entropy_coef != 0.0f)
+      hipLaunchKernelGGL((espo_policy_kernel<DT, W, true>), grid, block, lds, stream, ra, ro, rd, rq);
+    else
+      hipLaunchKernelGGL((espo_policy_kernel<DT, W, false>), grid, block, lds, stream, ra, ro, rd, rq);
+  }
 }
 
 // Log-probabilities, entropy and, if it is wanted, the gradient of the objective.

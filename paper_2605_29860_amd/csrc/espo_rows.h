@@ -170,6 +170,12 @@ __device__ __forceinline__ void rescale(SoftmaxSums& p, float m, float k2) {
   p.m = m;
 }
 
+// The same where one of the lanes needs it: after a row's first vectors hardly any does.
+template <bool kEntropy>
+__device__ __forceinline__ void follow(SoftmaxSums& p, float m, float k2) {
+  if (__builtin_amdgcn_ballot_w64(m > p.m) != 0) rescale<kEntropy>(p, m, k2);
+}
+
 template <bool kEntropy>
 __device__ __forceinline__ void add_logit(SoftmaxSums& p, float x, float k2) {
   float t = (x - p.m) * k2;
