@@ -208,22 +208,38 @@ __global__ __launch_bounds__(kGradThreads) void espo_logits_grad_kernel(RowArgs 
 // stored, its registers take that vector of the next row, from LDS or from memory.  So there is always something under way, also
 // where all compute units are at the same point, which they are more often than not.  The workgroups share the used rows
 // evenly, by rank among the used rows, and then the zeros of the unused ones, from the other end.
-constexpr int kHeld = 20;                        // vectors of a thread: 80 of the 128 registers that 16 waves per compute unit leave
+constexpr int kHeld = 19;                        // vectors of a thread: 76 of the 128 registers that 16 waves per compute unit leave
 constexpr int kStaged = 8;                       // of them through LDS: 128 KB of the compute unit's 160
-constexpr int kDealt = 1024;                     // rows of a workgroup
+constexpr int kDealt = 256;                      // rows of a workgroup
 constexpr int64_t kDealtEach = kDealt - 2;       // of both kinds together, rounded up each
+
+// 16 bytes per lane straight into LDS, the wave's 1024 bytes from `to` on (the same in all its lanes).  The compiler knows nothing of the load: who
+// reads what it brings waits for vmcnt(0) first, and the compiler's own waits for other loads come out as too long, never as too short.  (Of the
+// builtin for it it does know, and lets every load wait for all that are on their way.)
+__device__ __forceinline__ void load_to_lds(const char* from, const u32x4* to) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)to);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "memory", "m0");
+}
+
+// A workgroup's rows, and what belongs to the used ones: a load of these in the row loop would wait for all the logits on their way.
+struct DealtRows {
+  int32_t row[kDealt], token[kDealt];
+  TokenInputs in[kDealt];
+};
 
 // Keeps what was formed from a vector before from being kept in registers of its own (its logits as floats take twice the room).
 __device__ __forceinline__ void hold(u32x4& v) { asm volatile("" : "+v"(v)); }
 
 // The workgroup's share of the rows: the used ones from the front of `rows`, the others from its end, and how many of each.
 template <int W>
-__device__ __forceinline__ void deal_rows(const RowArgs& a, int32_t* rows, uint32_t (*counts)[W], int& nused, int& nother) {
+__device__ __forceinline__ void deal_rows(const RowArgs& a, const PolicyArgs& q, DealtRows& rows, uint32_t (*counts)[W], int& nused, int& nother) {
   const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, groups = gridDim.x, g = blockIdx.x, N = (uint32_t)a.N;
   uint32_t base = 0;                             // used rows so far
 #pragma unroll 1
   for (uint32_t row = 0; row < N; row += W * kWave) {
-    const bool mine = row + threadIdx.x < N, used = mine && used_row(a.tokens[row + threadIdx.x], a.V);
+    const bool mine = row + threadIdx.x < N;
+    const int32_t token = mine ? a.tokens[row + threadIdx.x] : -1;
+    const bool used = used_row(token, a.V);
     const uint64_t mask = __builtin_amdgcn_ballot_w64(used);
     uint32_t* count = counts[(row / (W * kWave)) & 1];
     if (lane == 0) count[wave] = (uint32_t)__builtin_popcountll(mask);
@@ -236,9 +252,14 @@ __device__ __forceinline__ void deal_rows(const RowArgs& a, int32_t* rows, uint3
     }
     const uint32_t other = row + threadIdx.x - rank;
     if (used) {
-      if (rank % groups == g) rows[rank / groups] = (int32_t)(row + threadIdx.x);
+      if (rank % groups == g) {
+        const uint32_t at = rank / groups;
+        rows.row[at] = (int32_t)(row + threadIdx.x);
+        rows.token[at] = token;
+        rows.in[at] = token_inputs(q, row + threadIdx.x);
+      }
     } else if (mine) {
-      if (other % groups == groups - 1 - g) rows[kDealt - 1 - other / groups] = (int32_t)(row + threadIdx.x);
+      if (other % groups == groups - 1 - g) rows.row[kDealt - 1 - other / groups] = (int32_t)(row + threadIdx.x);
     }
   }
   __syncthreads();
@@ -253,7 +274,8 @@ __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))
   extern __shared__ __align__(16) u32x4 staged[];  // [kStaged][kThreads]
   __shared__ SoftmaxSums lds[2][W];
   __shared__ uint32_t counts[2][W];
-  __shared__ int32_t rows[kDealt];
+  __shared__ DealtRows rows;
+  __shared__ float token_logit[2];
   const uint32_t nvec = (a.V + E - 1) / E;
   const int last = (int)((nvec - 1) / kThreads);  // of the vectors raw[0 .. last] of a thread, all but the last lie within the row
   // The thread's index, not to be seen through: its vectors' offsets would be kept in registers from row to row.
@@ -266,33 +288,29 @@ __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))
   // the row's last vector are that one.)
   const auto place = [&](const char* x, bool any, int r) { return x + (size_t)min((any ? r * kThreads : 0) + own_index(), nvec - 1) * 16; };
   int nused, nother;
-  deal_rows<W>(a, rows, counts, nused, nother);
-  const auto row_at = [&](int i) { return (int64_t)__builtin_amdgcn_readfirstlane(rows[i]); };
+  deal_rows<W>(a, q, rows, counts, nused, nother);
+  const auto row_at = [&](int i) { return (int64_t)__builtin_amdgcn_readfirstlane(rows.row[i]); };
   u32x4 raw[kHeld];
   {
     const char* x = a.logits + (nused > 0 ? row_at(0) : 0) * a.row_bytes;
 #pragma unroll
     for (int r = 0; r < kHeld; ++r) raw[r] = __builtin_nontemporal_load((const u32x4*)place(x, nused > 0, r));
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0), so that the loop's first vectors are waited for as LDS reads only
   }
 #pragma unroll 1
   for (int i = 0; i < nused; ++i) {
     const int64_t row = row_at(i);
     const bool more = i + 1 < nused;
-    const char* x = a.logits + row * a.row_bytes;
     const char* next_x = a.logits + row_at(more ? i + 1 : i) * a.row_bytes;
     char* out = d.dlogits + row * d.grad_bytes;
-    const int32_t token = a.tokens[row];
-    const float x_token = logit_at<DT>(x, (uint32_t)token);
-    const TokenInputs in = token_inputs(q, row);
-    __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): what the wave has read from `staged` has arrived
-#pragma unroll
-    for (int r = 0; r < kStaged; ++r)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)place(next_x, more, r),
-                                       (__attribute__((address_space(3))) void*)(staged + r * kThreads + (threadIdx.x & ~63u)), 16, 0, 0);
+    const int32_t token = __builtin_amdgcn_readfirstlane(rows.token[i]);
+    const int token_round = (int)((uint32_t)token / E / kThreads);
+    const bool holds_token = threadIdx.x == (uint32_t)token / E % kThreads;
     SoftmaxSums p{kMaskedRow, 0.0f, 0.0f};
     u32x4 tail = vec_masked<DT>();
 #pragma unroll
     for (int r = 0; r < kHeld; ++r) {
+      if (r == token_round && holds_token) token_logit[i & 1] = logit_in<DT>(raw[r], (uint32_t)token % E);
       if (r < last) {
         float y[E], m = p.m;
         hold(raw[r]);
@@ -305,6 +323,10 @@ __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))
       } else if (r == last) {
         tail = raw[r];
       }
+      // The first vectors have come from LDS and have been waited for, so their place there is free; and a load behind which these are issued
+      // would be waited for as if it were they.
+      if (r >= kStaged && r < 2 * kStaged)
+        load_to_lds(place(next_x, more, r - kStaged), staged + (r - kStaged) * kThreads + (threadIdx.x & ~(kWave - 1)));
     }
     const uint32_t last_vec = last * kThreads + own_index();
     {
@@ -322,11 +344,12 @@ __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))
     p = block_merge<W, true>(p, a.k2, lds[i & 1]);
     float logprob, entropy;
     float2 stats;
-    row_results(a, x_token, p, logprob, entropy, stats);
+    row_results(a, token_logit[i & 1], p, logprob, entropy, stats);
     if (threadIdx.x == 0) store_row(o, row, logprob, entropy, stats);
+    const TokenInputs in = rows.in[i];
     const Surrogate c = surrogate(q, in, logprob);
     const RowGrad g = row_grad(a, stats.x, stats.y, entropy, c.cut ? 0.0f : -in.weight * c.ratio * in.adv, kSlope ? -in.weight * q.entropy_coef : 0.0f);
-    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0): the wave's part of `staged` is there
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the wave's part of `staged` is there
 #pragma unroll
     for (int r = 0; r < kHeld; ++r) {
       hold(raw[r]);
@@ -334,11 +357,14 @@ __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))
         const uint32_t at = r * kThreads + own_index();
         __builtin_nontemporal_store(grad_vec<DT, kSlope>(a, g, raw[r], at, token), (u32x4*)(out + (size_t)at * 16));
       }
-      raw[r] = r < kStaged ? staged[r * kThreads + own_index()] : __builtin_nontemporal_load((const u32x4*)place(next_x, more, r));
+      if (r < kStaged)
+        raw[r] = staged[r * kThreads + own_index()];
+      else
+        raw[r] = __builtin_nontemporal_load((const u32x4*)place(next_x, more, r));
     }
     if (last_vec < nvec) vec_store<DT>(out, last_vec, a.V, grad_vec<DT, kSlope>(a, g, tail, last_vec, token));
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);            // the last loads, of no row
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the last loads, of no row
 #pragma unroll 1
   for (int i = 0; i < nother; ++i) {
     const int64_t row = row_at(kDealt - 1 - i);
@@ -420,7 +446,7 @@ RowArgs rows_from(RowArgs a, int64_t from, int64_t n) {
 template <int DT, int W>
 void policy_held(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, hipStream_t stream) {
   const int64_t groups = a.N < kComputeUnits * (16 / W) ? a.N : kComputeUnits * (16 / W);
-  for (int64_t from = 0; from < a.N; from += groups * kDealtEach) {  // one launch up to 261632 rows
+  for (int64_t from = 0; from < a.N; from += groups * kDealtEach) {  // one launch up to 65024 rows
     const int64_t n = a.N - from < groups * kDealtEach ? a.N - from : groups * kDealtEach;
     const RowArgs ra = rows_from(a, from, n);
     const RowOutputs ro{o.logprob + from, o.entropy + from, o.stats + from};

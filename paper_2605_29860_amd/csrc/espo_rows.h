@@ -35,6 +35,20 @@ __device__ __forceinline__ void vec_unpack(u32x4 r, float x[vec_elems<DT>()]) {
   }
 }
 
+// Logit j of a vector.
+template <int DT>
+__device__ __forceinline__ float logit_in(u32x4 raw, uint32_t j) {
+  const uint32_t q = DT == ESPO_BF16 ? j >> 1 : j;
+  uint32_t w = raw[0];
+#pragma unroll
+  for (uint32_t i = 1; i < 4; ++i) {
+    const uint32_t wi = raw[i];
+    w = q == i ? wi : w;
+  }
+  if constexpr (DT == ESPO_BF16) w = j & 1 ? w & 0xffff0000u : w << 16;
+  return __builtin_bit_cast(float, w);
+}
+
 // Rounded once, to the nearest even.
 template <int DT>
 __device__ __forceinline__ u32x4 vec_pack(const float x[vec_elems<DT>()]) {

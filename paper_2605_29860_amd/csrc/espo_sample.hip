@@ -228,20 +228,6 @@ __device__ __forceinline__ void logits_of(const Row& r, uint32_t i, u32x4 raw, f
   }
 }
 
-// Logit j of a vector.
-template <int DT>
-__device__ __forceinline__ float logit_in(u32x4 raw, uint32_t j) {
-  const uint32_t q = DT == ESPO_BF16 ? j >> 1 : j;
-  uint32_t w = raw[0];
-#pragma unroll
-  for (uint32_t i = 1; i < 4; ++i) {
-    const uint32_t wi = raw[i];
-    w = q == i ? wi : w;
-  }
-  if constexpr (DT == ESPO_BF16) w = j & 1 ? w & 0xffff0000u : w << 16;
-  return __builtin_bit_cast(float, w);
-}
-
 template <int E>
 __device__ __forceinline__ float max_of(const float y[E]) {
   float m = y[0];
