@@ -7,13 +7,17 @@
 // weights and sums are doubles (a v_fma_f64 takes no longer than a v_fma_f32 here), and sums that are formed by atomics are integers
 // (the order of additions then changes nothing).
 //
-// One workgroup per row, which is streamed once.  A row without filters leaves the sum of each wave's part; the part, the tile and
-// the vector that the draw falls into are read again.  A filtered row leaves how many logits (and, of fp32 logits under top-p, how
-// much mass) fall into each of 4355 bins, which are the bf16 numbers from 2^-10 to 128 of either sign, and the largest logit of
-// every block of 16 vectors.  The bins say where the cut is: exactly so for bf16 logits, whose bins hold one value each, and up to one
-// bin's members for fp32 logits, which are then collected and ranked.  Only blocks that reach the cut are read again.
-// Rows that the bins do not describe (logits of 128 and more, a cut among the numbers next to 0, a nucleus that -128 still has a
-// share in, a bin with thousands of members) find their cut by three levels of 2048 bins over the whole key, one pass over the row each.
+// One workgroup per row, which is streamed once.  A row without filters leaves the sum of every chunk of four tiles; the chunk that the
+// draw falls into is read again.  A filtered row leaves how many logits (and, of fp32 logits under top-p, how much mass) fall into
+// each of 4355 bins, which are the bf16 numbers from 2^-10 to 128 of either sign, and the largest logit of every block of 16
+// vectors.  The bins say where the cut is: exactly so for bf16 logits, whose bins hold one value each, and up to one bin's
+// members for fp32 logits, which are then collected and ranked.  Only blocks that reach the cut are read again, or, where those
+// are many, the row.  Rows that the bins do not describe (logits of 128 and more, a nucleus that -128 still has a share in, a bin with
+// hundreds of members) find their cut by three levels of 2048 bins over the whole key, one pass over the row each.
+//
+// What follows the stream is a chain of short steps that run once per row, and what they cost is the fetching of their instructions: a first
+// version that unrolled them took 7 us for each of cut, second reading and draw, at any batch size.  So they are loops, of one
+// instance of each thing.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -28,7 +32,7 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kAhead = 4;                   // vectors of a lane in flight
+constexpr int kChunk = 4;                   // tiles of a chunk, the unit of a pass that sums weights
 constexpr int kBlockVecs = 16;              // vectors of a block: one row of 16 lanes, whose maximum takes four DPP steps
 constexpr double kFixed = 8796093022208.0;  // 2^43: a weight of 1 as an integer; 2^20 of them stay below 2^63
 constexpr double kNoWeight = 1e-250;        // weights below this count as none
@@ -102,9 +106,7 @@ struct SampleArgs {
   uint32_t lds_blocks, lds_members;  // where the blocks' maxima and a bin's members start in dynamic LDS
 };
 
-struct Row {
-  const char* x;
-  uint32_t V, nvec, ntiles;
+struct Row : RowView {
   double c, inv_t, m;  // log2(e) / T, 1 / T, largest logit
   __device__ __forceinline__ double weight(float v) const { return exp2_f64(((double)v - m) * c); }
 };
@@ -114,19 +116,21 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float of_key(uint32_t key) { return __builtin_bit_cast(float, key >> 31 ? key & 0x7fffffffu : ~key); }
 
 constexpr int kLevelBins = 2048;            // of a level of the search over whole keys: 11, 11 and 10 bits
 constexpr int kMostMembers = 512;           // of a bin that are ranked, each against all others
+constexpr uint32_t kMostRounds = 4;         // of the workgroup over the blocks that are visited; beyond that the row is streamed again
 
 template <int W>
 struct SampleShared {
-  double part[4096 / W + 1];  // sums of the tiles of a wave's part
-  double wave_f64[W];
+  double wave_f64[3][W];
   u64 found_mass, above_mass, kept_mass;
-  float m[W];
-  uint32_t at[W], wave_u32[W];
-  uint32_t found_bin, above_count, first, last, nmembers, cut_key;
   double rest;
+  float m[W];
+  int2 picks[3][W];
+  uint32_t at[W], wave_u32[W];
+  uint32_t found_bin, above_count, nmembers, cut_key;
 };
 
 // The inclusive sums over the lanes before and at this one.
@@ -149,82 +153,72 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
   return v;
 }
 __device__ __forceinline__ u64 wave_scan(u64 v) {
-#pragma unroll
+#pragma unroll 1
   for (int d = 1; d < kWave; d *= 2) {
     const u64 o = __shfl_up(v, d);
     if ((int)(threadIdx.x & (kWave - 1)) >= d) v += o;
   }
   return v;
 }
+__device__ __forceinline__ double lane_f64(double v, int lane) {  // the same lane in the whole wave
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
 
 // The sum over the threads before this one, and over all of them; lds: W entries that a barrier has freed.
-template <int W, typename T>
-__device__ __forceinline__ T block_before(T v, T* lds, T& total) {
-  const int wave = threadIdx.x >> 6;
-  const T upto = wave_scan(v);
-  if ((threadIdx.x & (kWave - 1)) == kWave - 1) lds[wave] = upto;
+template <int W>
+__device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* lds, uint32_t& total) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const uint32_t upto = wave_scan(v);
+  if (lane == kWave - 1) lds[wave] = upto;
   __syncthreads();
-  T before = 0, all = 0;
-#pragma unroll
-  for (int i = 0; i < W; ++i) {
-    const T each = lds[i];
-    if (i < wave) before += each;
-    all += each;
-  }
-  total = all;
-  return before + upto - v;
+  const uint32_t all = wave_scan(lane < W ? lds[lane] : 0u);
+  total = (uint32_t)__builtin_amdgcn_readlane((int)all, kWave - 1);
+  return upto - v + (wave > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)all, wave - 1) : 0u);
+}
+template <int W>
+__device__ __forceinline__ double block_before(double v, double* lds, double& total) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const double upto = wave_scan(v);
+  if (lane == kWave - 1) lds[wave] = upto;
+  __syncthreads();
+  const double all = wave_scan(lane < W ? lds[lane] : 0.0);
+  total = lane_f64(all, kWave - 1);
+  return upto - v + (wave > 0 ? lane_f64(all, wave - 1) : 0.0);
 }
 
 // The thread whose part [before, before + v) of a running sum holds `target`: the first with before + v beyond it (or, where `reach`,
-// at it); the last with any part if rounding leaves none.  The same in all threads; s.first and s.last have been reset before a barrier.
+// at it); the last with any part if rounding leaves none.  The same in all threads.  (By ballots: LDS atomics on one word are turned into a
+// loop over the lanes, 4 us here.)
 template <int W>
-__device__ __forceinline__ uint32_t block_pick(double before, double v, double least, double target, bool reach, SampleShared<W>& s) {
-  if (v > least) {
-    const double upto = before + v;
-    if (upto > target || (reach && upto == target)) atomicMin(&s.first, threadIdx.x);
-    atomicMax(&s.last, threadIdx.x);
-  }
+__device__ __forceinline__ uint32_t block_pick(double before, double v, double target, bool reach, int2* lds) {
+  const double upto = before + v;
+  const int lane = threadIdx.x & (kWave - 1);
+  const bool any = v > kNoWeight;
+  const uint64_t hit = __builtin_amdgcn_ballot_w64(any && (upto > target || (reach && upto == target))), some = __builtin_amdgcn_ballot_w64(any);
+  const int base = (int)(threadIdx.x - lane);
+  if (lane == 0) lds[threadIdx.x >> 6] = int2{hit ? base + (int)__builtin_ctzll(hit) : -1, some ? base + 63 - (int)__builtin_clzll(some) : -1};
   __syncthreads();
-  return s.first != 0xffffffffu ? s.first : s.last;
+  const int2 w = lane < W ? lds[lane] : int2{-1, -1};
+  const uint64_t hits = __builtin_amdgcn_ballot_w64(w.x >= 0), somes = __builtin_amdgcn_ballot_w64(w.y >= 0);
+  if (hits) return (uint32_t)__builtin_amdgcn_readlane(w.x, (int)__builtin_ctzll(hits));
+  return somes ? (uint32_t)__builtin_amdgcn_readlane(w.y, 63 - (int)__builtin_clzll(somes)) : 0u;
 }
 
-// Calls use(tile, vector) for tiles first, first + step, ... below end, kAhead of them in flight while the kAhead before are used.
-// A vector's index is clamped to the row's last one; `use` looks at what lies beyond V.
+// Calls use(t, raw) for tiles first, first + step, ... below end, one after the other, with the next three on their way: a loop of little
+// code.  Every load is in bounds (see stream_tiles); tile_logits masks what lies beyond V.
 template <typename Use>
-__device__ __forceinline__ void stream(const Row& r, uint32_t first, uint32_t end, uint32_t step, Use&& use) {
+__device__ __forceinline__ void stream_ring(const RowView& r, uint32_t first, uint32_t end, uint32_t step, Use&& use) {
   const uint32_t lane = threadIdx.x & (kWave - 1);
   const auto load = [&](uint32_t t) {
-    return __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min(t * kWave + lane, r.nvec - 1) * 16));
+    return __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min(min(t, end - 1) * kWave + lane, r.nvec - 1) * 16));
   };
   if (first >= end) return;
-  u32x4 cur[kAhead], nxt[kAhead];
-#pragma unroll
-  for (int j = 0; j < kAhead; ++j) cur[j] = load(first + j * step);
-  for (uint32_t t = first; t < end; t += kAhead * step) {
-    const bool more = t + kAhead * step < end;
-    if (more) {
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) nxt[j] = load(t + (kAhead + j) * step);
-    }
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (t + j * step < end) use(t + j * step, cur[j]);
-    if (more) {
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) cur[j] = nxt[j];
-    }
-  }
-}
-
-// A vector's logits; those at or beyond V are masked.
-template <int DT>
-__device__ __forceinline__ void logits_of(const Row& r, uint32_t i, u32x4 raw, float y[vec_elems<DT>()]) {
-  constexpr uint32_t E = vec_elems<DT>();
-  vec_unpack<DT>(raw, y);
-  if (i * E + E > r.V) {
-#pragma unroll
-    for (uint32_t j = 0; j < E; ++j)
-      if (i * E + j >= r.V) y[j] = kNegInf;
+  u32x4 a = load(first), b = load(first + step), c = load(first + 2 * step), d = load(first + 3 * step);
+#pragma unroll 1
+  for (uint32_t t = first; t < end; t += step) {
+    const u32x4 raw = a;
+    a = b, b = c, c = d, d = load(t + 4 * step);
+    use(t, raw);
   }
 }
 
@@ -271,13 +265,10 @@ __device__ __forceinline__ uint32_t find_cut(const Row& r, uint32_t floor, const
     __syncthreads();
 #pragma unroll 1
     for (uint32_t i = threadIdx.x; i < r.nvec; i += W * kWave) {
-      float y[E];
-      vec_unpack<DT>(vec_load<DT>(r.x, i, r.V), y);
+      const u32x4 raw = vec_load<DT>(r.x, i, r.V);
 #pragma unroll 1
       for (uint32_t j = 0; j < E; ++j) {
-        float x = y[0];
-#pragma unroll
-        for (uint32_t k = 1; k < E; ++k) x = j == k ? y[k] : x;
+        const float x = logit_in<DT>(raw, j);
         const uint32_t key = key_of(x);
         if (!(x > kMaskedRow) || key < floor || (level > 0 && (key >> (shift + bits)) != prefix)) continue;
         const uint32_t bin = (key >> shift) & ((1u << bits) - 1);
@@ -323,78 +314,80 @@ __device__ __forceinline__ uint32_t find_cut(const Row& r, uint32_t floor, const
 }
 
 // ---------------------------------------------------------------- the draw
-// The lane at which the running sum of v exceeds `rest`, or the last one with any weight; `rest` becomes what is left before it.
-__device__ __forceinline__ int pick_lane(double v, double& rest) {
-  const double upto = wave_scan(v);
-  const uint64_t hit = __builtin_amdgcn_ballot_w64(v > kNoWeight && upto > rest), some = __builtin_amdgcn_ballot_w64(v > kNoWeight);
-  const int lane = hit ? (int)__builtin_ctzll(hit) : 63 - (int)__builtin_clzll(some | 1);
-  rest -= __shfl(upto - v, lane);
-  return lane;
-}
-
 __device__ __forceinline__ void store_result(const SampleArgs& a, int64_t b, int32_t token, float logprob) {
   a.tokens[b] = token;
   if (a.logprob) a.logprob[b] = logprob;
 }
 
-// The draw among one vector per lane of a wave, starting at vector i0: `rest` of the running sum is left before it.
-template <int DT, typename Kept>
-__device__ __forceinline__ void draw_in_vectors(const SampleArgs& a, int64_t b, const Row& r, uint32_t i, bool mine, double rest, double total,
-                                                Kept&& kept) {
-  constexpr uint32_t E = vec_elems<DT>();
-  const u32x4 raw = mine ? vec_load<DT>(r.x, i, r.V) : vec_masked<DT>();
-  const double ln_total = log(total);       // while the load is on its way
-  float y[E];
-  vec_unpack<DT>(raw, y);
-  double w[E], sum = 0.0;
-#pragma unroll
-  for (uint32_t j = 0; j < E; ++j) sum += w[j] = kept(y[j]);
-  const int who = pick_lane(sum, rest);
-  if ((int)(threadIdx.x & (kWave - 1)) != who) return;
-  int32_t token = -1;
-  float x = 0.0f;
-  double upto = 0.0;
-  bool found = false;
-#pragma unroll
-  for (uint32_t j = 0; j < E; ++j) {
-    if (found || !(w[j] > 0.0)) continue;
-    token = (int32_t)(i * E + j), x = y[j];
-    upto += w[j];
-    found = upto > rest;
-  }
-  store_result(a, b, token, (float)(((double)x - r.m) * r.inv_t - ln_total));
+// ln v for a normal number: the hardware's logarithm of the mantissa, and one step of Newton's method.
+__device__ __forceinline__ double log_f64(double v) {
+  const int e = ((__double2hiint(v) >> 20) & 0x7ff) - 1023;
+  const double f = __hiloint2double(__double2hiint(v) - (int)((uint32_t)e << 20), __double2loint(v));  // in [1, 2)
+  const double y = (double)__builtin_amdgcn_logf((float)f);
+  return (y + (double)e) * 0.693147180559945309 + (f * exp2_f64(-y) - 1.0);
 }
 
-// The draw within tiles t0 .. t1 - 1, where the running sum falls: the tiles' sums, the tile, its vectors.
-template <int DT, int W, typename Kept>
-__device__ __forceinline__ void draw_in_tiles(const SampleArgs& a, int64_t b, const Row& r, uint32_t t0, uint32_t t1, double rest, double total,
-                                              SampleShared<W>& s, Kept&& kept) {
-  constexpr uint32_t E = vec_elems<DT>();
-  const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
-  stream(r, t0 + wave, t1, W, [&](uint32_t t, u32x4 raw) {
-    const uint32_t i = t * kWave + lane;
-    float y[E];
-    logits_of<DT>(r, i, raw, y);
-    double w = 0.0;
-#pragma unroll
-    for (uint32_t j = 0; j < E; ++j) w += kept(y[j]);
-    w = wave_sum_f64(w);
-    if (lane == 0) s.part[t - t0] = w;
-  });
-  __syncthreads();
-  if (wave != 0) return;
-  uint32_t tile = t0;
-  double left = rest;
-#pragma unroll 1
-  for (uint32_t t = t0; t < t1; t += kWave) {
-    const double w = t + lane < t1 ? s.part[t + lane - t0] : 0.0, all = wave_sum_f64(w);
-    if (!(all > kNoWeight)) continue;
-    left = rest;
-    tile = t + (uint32_t)pick_lane(w, left);
-    if (all > rest) break;
-    rest -= all;
+// What is kept of a row, as far as it is known.
+struct Kept {
+  float cut;    // logits of at least this
+  double min_p; // weights of at least this
+  __device__ __forceinline__ double weight(const Row& r, float x) const {
+    if (!(x >= cut) || !(x > kMaskedRow)) return 0.0;
+    const double w = r.weight(x);
+    return w >= min_p ? w : 0.0;
   }
-  draw_in_vectors<DT>(a, b, r, tile * kWave + lane, true, left, total, kept);
+};
+
+// The draw from n sums over `span` consecutive vectors each, the q-th of them starting at start(q): the one that the draw falls
+// into, its vector, its logit.  A barrier has passed since the sums were stored.
+template <int DT, int W, typename Start>
+__device__ __forceinline__ void draw(const SampleArgs& a, int64_t b, const Row& r, const Kept& keep, const double* sums, uint32_t n, uint32_t span,
+                                     SampleShared<W>& s, Start&& start) {
+  constexpr uint32_t E = vec_elems<DT>(), kThreads = W * kWave;
+  const uint32_t each = (n + kThreads - 1) / kThreads, q0 = threadIdx.x * each, q1 = min(q0 + each, n);
+  double mine = 0.0, total;
+#pragma unroll 1
+  for (uint32_t q = q0; q < q1; ++q) mine += sums[q];
+  double before = block_before<W>(mine, s.wave_f64[1], total);
+  const double target = (double)a.u[b] * total;
+  if (threadIdx.x == block_pick<W>(before, mine, target, false, s.picks[1])) {
+    double rest = target - before;
+    uint32_t at = q0;
+#pragma unroll 1
+    for (uint32_t q = q0; q < q1; ++q) {
+      const double w = sums[q];
+      if (!(w > kNoWeight)) continue;
+      at = q;
+      s.rest = rest;
+      if (w > rest) break;
+      rest -= w;
+    }
+    s.found_bin = start(at);
+  }
+  __syncthreads();
+  const uint32_t i = s.found_bin + threadIdx.x;
+  const u32x4 raw = threadIdx.x < span ? vec_load<DT>(r.x, i, r.V) : vec_masked<DT>();
+  const double ln_total = log_f64(total);   // while the load is on its way
+  mine = 0.0;
+  if (threadIdx.x < span) {
+#pragma unroll 1
+    for (uint32_t j = 0; j < E; ++j) mine += keep.weight(r, logit_in<DT>(raw, j));
+  }
+  double all;
+  before = block_before<W>(mine, s.wave_f64[2], all);
+  if (threadIdx.x != block_pick<W>(before, mine, s.rest, false, s.picks[2])) return;
+  int32_t token = -1;
+  float x = 0.0f;
+#pragma unroll 1
+  for (uint32_t j = 0; j < E; ++j) {
+    const float xj = logit_in<DT>(raw, j);
+    const double w = keep.weight(r, xj);
+    if (!(w > 0.0)) continue;
+    token = (int32_t)(i * E + j), x = xj;
+    before += w;
+    if (before > s.rest) break;
+  }
+  store_result(a, b, token, (float)(((double)x - r.m) * r.inv_t - ln_total));
 }
 
 // Greedy: the first index of the largest logit.
@@ -404,16 +397,16 @@ __device__ __forceinline__ void greedy(const SampleArgs& a, int64_t b, const Row
   const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   float m = kMaskedRow;
   uint32_t at = 0xffffffffu;
-  stream(r, wave, r.ntiles, W, [&](uint32_t t, u32x4 raw) {
-    const uint32_t i = t * kWave + lane;
+  stream_ring(r, wave, r.ntiles, W, [&](uint32_t t, u32x4 raw) {
     float y[E];
-    logits_of<DT>(r, i, raw, y);
+    tile_logits<DT>(r, t, raw, y);
     const float top = max_of<E>(y);
     if (top > m) {
       m = top;
+      const uint32_t i = t * kWave + lane;
 #pragma unroll
       for (int j = E - 1; j >= 0; --j)
-        if (y[j] == top && i * E + j < r.V) at = i * E + j;
+        if (y[j] == top) at = i * E + j;
     }
   });
   const float top = wave_max(m);
@@ -427,81 +420,114 @@ __device__ __forceinline__ void greedy(const SampleArgs& a, int64_t b, const Row
   if (lane == 0) store_result(a, b, all > kMaskedRow ? (int32_t)at : -1, 0.0f);
 }
 
-// No filter: each wave sums its part of the row, relative to a reference of its own that follows the largest logit only when that
-// runs 2^500 ahead.
-template <int DT, int W>
-__device__ __forceinline__ void draw_plain(const SampleArgs& a, int64_t b, Row& r, SampleShared<W>& s) {
-  constexpr uint32_t E = vec_elems<DT>();
-  const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, per = (r.ntiles + W - 1) / W;
-  float m = kMaskedRow, limit = kMaskedRow;
-  double sum = 0.0, ref = 0.0;
-  const float lead = (float)(500.0 / r.c);
-  stream(r, wave * per, min((wave + 1) * per, r.ntiles), 1, [&](uint32_t t, u32x4 raw) {
-    const uint32_t i = t * kWave + lane;
-    float y[E];
-    logits_of<DT>(r, i, raw, y);
-    const float top = max_of<E>(y);
-    m = fmaxf(m, top);
-    if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
-      const float to = wave_max(m);
-      sum = limit > kMaskedRow ? sum * exp2_f64((ref - (double)to) * r.c) : 0.0;
-      ref = (double)to;
-      limit = to + lead;
-    }
+// Chunks of a row: kChunk tiles each, a wave takes every W-th.  Calls use(t, raw) for a chunk's tiles and done(chunk) after them.
+template <int W, typename Use, typename Done>
+__device__ __forceinline__ void stream_chunks(const RowView& r, Use&& use, Done&& done) {
+  const uint32_t lane = threadIdx.x & (kWave - 1), chunks = (r.ntiles + kChunk - 1) / kChunk;
+  const auto load = [&](uint32_t c, uint32_t j) {
+    return __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min((min(c, chunks - 1) * kChunk + j) * kWave + lane, r.nvec - 1) * 16));
+  };
+  uint32_t c = threadIdx.x >> 6;
+  if (c >= chunks) return;
+  u32x4 cur[kChunk], nxt[kChunk];
 #pragma unroll
-    for (uint32_t j = 0; j < E; ++j) sum += exp2_f64(((double)y[j] - ref) * r.c);
-  });
+  for (uint32_t j = 0; j < kChunk; ++j) cur[j] = load(c, j);
+#pragma unroll 1
+  for (; c < chunks; c += W) {
+#pragma unroll
+    for (uint32_t j = 0; j < kChunk; ++j) nxt[j] = load(c + W, j);
+#pragma unroll
+    for (uint32_t j = 0; j < kChunk; ++j)
+      if (c * kChunk + j < r.ntiles) use(c * kChunk + j, cur[j]);
+    done(c);
+#pragma unroll
+    for (uint32_t j = 0; j < kChunk; ++j) cur[j] = nxt[j];
+  }
+}
+
+// No filter: the sum of every chunk, relative to a reference that follows the wave's largest logit only when that runs 2^500 ahead.
+template <int DT, int W>
+__device__ __forceinline__ void draw_plain(const SampleArgs& a, int64_t b, Row& r, unsigned char* lds, SampleShared<W>& s) {
+  constexpr uint32_t E = vec_elems<DT>(), kThreads = W * kWave;
+  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
+  double* sums = (double*)lds;
+  float* refs = (float*)(sums + chunks);
+  float m = kMaskedRow, ref = kMaskedRow, limit = kMaskedRow;
+  double sum = 0.0;
+  const float lead = (float)(500.0 / r.c);
+  stream_chunks<W>(
+      r,
+      [&](uint32_t t, u32x4 raw) {
+        float y[E];
+        tile_logits<DT>(r, t, raw, y);
+        const float top = max_of<E>(y);
+        m = fmaxf(m, top);
+        if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
+          const float to = wave_max(m);
+          sum = limit > kMaskedRow ? sum * exp2_f64(((double)ref - (double)to) * r.c) : 0.0;
+          ref = to;
+          limit = to + lead;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < E; ++j) sum += exp2_f64(((double)y[j] - (double)ref) * r.c);
+      },
+      [&](uint32_t c) {
+        sum = wave_sum_f64(sum);
+        if (threadIdx.x % kWave == 0) sums[c] = sum, refs[c] = ref;
+        sum = 0.0;
+      });
   const float top = block_max<W>(m, s);
   if (!(top > kMaskedRow)) {
     if (threadIdx.x == 0) store_result(a, b, -1, 0.0f);
     return;
   }
   r.m = (double)top;
-  sum = limit > kMaskedRow ? wave_sum_f64(sum) * exp2_f64((ref - r.m) * r.c) : 0.0;
-  if (lane == 0) s.wave_f64[wave] = sum;
+#pragma unroll 1
+  for (uint32_t c = threadIdx.x; c < chunks; c += kThreads) sums[c] = refs[c] > kMaskedRow ? sums[c] * exp2_f64(((double)refs[c] - r.m) * r.c) : 0.0;
   __syncthreads();
-  const double each = lane < W ? s.wave_f64[lane] : 0.0, total = wave_sum_f64(each);
-  double rest = (double)a.u[b] * total;
-  const uint32_t seg = (uint32_t)pick_lane(each, rest);
-  draw_in_tiles<DT, W>(a, b, r, seg * per, min((seg + 1) * per, r.ntiles), rest, total, s,
-                       [&](float x) { return x > kMaskedRow ? r.weight(x) : 0.0; });
+  draw<DT, W>(a, b, r, Kept{-3.402823466e38f, 0.0}, sums, chunks, kChunk * kWave, s, [](uint32_t q) { return q * (kChunk * kWave); });
 }
 
-// A filtered row whose cut the bins do not give: the cut by whole keys, then the sum of each wave's part.
+// Of many kept logits: the kept sum of every chunk, with the cut and the largest logit known.
 template <int DT, int W>
-__device__ __forceinline__ void draw_by_keys(const SampleArgs& a, int64_t b, const Row& r, int32_t k, float p, double min_p, unsigned char* lds,
-                                             SampleShared<W>& s) {
+__device__ __forceinline__ void draw_many(const SampleArgs& a, int64_t b, const Row& r, const Kept& keep, unsigned char* lds, SampleShared<W>& s) {
   constexpr uint32_t E = vec_elems<DT>();
-  const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, per = (r.ntiles + W - 1) / W;
+  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
+  double* sums = (double*)lds;
+  double sum = 0.0;
+  __syncthreads();                          // what was in LDS has been read
+  stream_chunks<W>(
+      r,
+      [&](uint32_t t, u32x4 raw) {
+        float y[E];
+        tile_logits<DT>(r, t, raw, y);
+        uint32_t in = 0;
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e) in |= y[e] >= keep.cut && y[e] > kMaskedRow ? 1u << e : 0u;
+        for (; in != 0; in &= in - 1) sum += keep.weight(r, logit_in<DT>(raw, (uint32_t)__builtin_ctz(in)));
+      },
+      [&](uint32_t c) {
+        sum = wave_sum_f64(sum);
+        if (threadIdx.x % kWave == 0) sums[c] = sum;
+        sum = 0.0;
+      });
+  __syncthreads();
+  draw<DT, W>(a, b, r, keep, sums, chunks, kChunk * kWave, s, [](uint32_t q) { return q * (kChunk * kWave); });
+}
+
+// The cut of a row that the bins do not describe.
+template <int DT, int W>
+__device__ __forceinline__ float cut_by_keys(const Row& r, int32_t k, float p, unsigned char* lds, SampleShared<W>& s) {
   uint32_t floor = 0;
   u64 mass = 0;
 #pragma unroll 1
-  for (int pass = 0; pass < 2; ++pass) {  // the k largest (or the mass of the whole row), then the nucleus
-    if (pass == 0 && k == 0 && p == 0.0f) continue;
+  for (int pass = 0; pass < 2; ++pass) {    // the k largest (or the mass of the whole row), then the nucleus
     if (pass == 1 && p == 0.0f) continue;
     const Goal goal = pass == 1 ? Goal{false, 0, (double)p * (double)mass} : Goal{true, k > 0 ? (u64)k : (u64)r.V + 1, 0.0};
     const uint32_t cut = find_cut<DT, W>(r, floor, goal, lds, s, mass);
     if (pass == 1 || k > 0) floor = cut;
   }
-  const auto kept = [&](float x) {
-    if (!(x > kMaskedRow) || key_of(x) < floor) return 0.0;
-    const double w = r.weight(x);
-    return w >= min_p ? w : 0.0;
-  };
-  double sum = 0.0;
-  stream(r, wave * per, min((wave + 1) * per, r.ntiles), 1, [&](uint32_t t, u32x4 raw) {
-    float y[E];
-    logits_of<DT>(r, t * kWave + lane, raw, y);
-#pragma unroll
-    for (uint32_t j = 0; j < E; ++j) sum += kept(y[j]);
-  });
-  sum = wave_sum_f64(sum);
-  if (lane == 0) s.wave_f64[wave] = sum;
-  __syncthreads();
-  const double each = lane < W ? s.wave_f64[lane] : 0.0, total = wave_sum_f64(each);
-  double rest = (double)a.u[b] * total;
-  const uint32_t seg = (uint32_t)pick_lane(each, rest);
-  draw_in_tiles<DT, W>(a, b, r, seg * per, min((seg + 1) * per, r.ntiles), rest, total, s, kept);
+  return of_key(floor);
 }
 
 // Collects the logits of one bin; false if there are more than are ranked.
@@ -543,17 +569,19 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
   float* members = (float*)(lds + a.lds_members);
   const bool counts = k > 0 || (kOne && p > 0.0f), masses = !kOne && p > 0.0f;
 
-  for (int i = threadIdx.x; i < kBins; i += kThreads) {
-    count[i] = 0;
-    if (masses) mass[i] = 0;
+  if (counts || masses) {
+#pragma unroll 1
+    for (int i = threadIdx.x; i < kBins; i += kThreads) {
+      count[i] = 0;
+      if (masses) mass[i] = 0;
+    }
+    __syncthreads();
   }
-  if (threadIdx.x == 0) s.first = 0xffffffffu, s.last = 0, s.found_bin = 0;
-  __syncthreads();
   float m = kMaskedRow;
   double next_to_0 = 0.0;                   // mass of bf16 logits next to 0, relative to e^0
-  stream(r, wave, r.ntiles, W, [&](uint32_t t, u32x4 raw) {
+  stream_ring(r, wave, r.ntiles, W, [&](uint32_t t, u32x4 raw) {
     float y[E];
-    logits_of<DT>(r, t * kWave + lane, raw, y);
+    tile_logits<DT>(r, t, raw, y);
     float top = max_of<E>(y);
     m = fmaxf(m, top);
     ESPO_DPP_STEP("v_max_f32", top, "row_shr:1 row_mask:0xf bank_mask:0xf");
@@ -562,33 +590,27 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
     ESPO_DPP_STEP("v_max_f32", top, "row_shr:8 row_mask:0xf bank_mask:0xf");
     if (lane % kBlockVecs == kBlockVecs - 1) blocks[t * (kWave / kBlockVecs) + lane / kBlockVecs] = top;
     if (counts) {
-      if constexpr (kOne) {
-        float low = y[0], least = fabsf(y[0]);
+      float low = y[0], least = fabsf(y[0]);
 #pragma unroll
-        for (uint32_t j = 1; j < E; ++j) low = fminf(low, y[j]), least = fminf(least, fabsf(y[j]));
-        const bool all = __builtin_amdgcn_ballot_w64(!(low > -kBinsBelow)) == 0;
+      for (uint32_t j = 1; j < E; ++j) low = fminf(low, y[j]), least = fminf(least, fabsf(y[j]));
+      if (kOne && __builtin_amdgcn_ballot_w64(!(low > -kBinsBelow)) == 0) {
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
           const uint32_t at = bins_of_pair<4>(raw[j]);
-          if (all) {
-            atomicAdd((uint32_t*)(lds + (at & 0xffffu)), 1u);
-            atomicAdd((uint32_t*)(lds + (at >> 16)), 1u);
-          } else {                          // masked logits would all wait for one counter
-            if (y[2 * j] > -kBinsBelow) atomicAdd((uint32_t*)(lds + (at & 0xffffu)), 1u);
-            if (y[2 * j + 1] > -kBinsBelow) atomicAdd((uint32_t*)(lds + (at >> 16)), 1u);
-          }
+          atomicAdd((uint32_t*)(lds + (at & 0xffffu)), 1u);
+          atomicAdd((uint32_t*)(lds + (at >> 16)), 1u);
         }
-        if (p > 0.0f && __builtin_amdgcn_ballot_w64(least < 0x1p-10f) != 0) {
-#pragma unroll 1
-          for (uint32_t j = 0; j < E; ++j) {
-            const float v = logit_in<DT>(raw, j);
-            if (fabsf(v) < 0x1p-10f) next_to_0 += exp2_f64((double)v * r.c);
-          }
-        }
-      } else {
+      } else {                              // masked logits would all wait for one counter
 #pragma unroll
         for (uint32_t j = 0; j < E; ++j)
           if (y[j] > -kBinsBelow) atomicAdd(&count[bin_of(__builtin_bit_cast(uint32_t, y[j]))], 1u);
+      }
+      if (kOne && p > 0.0f && __builtin_amdgcn_ballot_w64(least < 0x1p-10f) != 0) {
+#pragma unroll 1
+        for (uint32_t j = 0; j < E; ++j) {
+          const float v = logit_in<DT>(raw, j);
+          if (fabsf(v) < 0x1p-10f && (t * kWave + lane) * E + j < r.V) next_to_0 += exp2_f64((double)v * r.c);
+        }
       }
     }
     if (masses) {
@@ -616,27 +638,25 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
                (top < kBinsBelow && (!masses || (double)top * r.inv_t < 300.0) && (p == 0.0f || r.inv_t < 300000.0) &&
                 (p == 0.0f || k > 0 || ((double)top + kBinsBelow) * r.inv_t > 50.0));
   constexpr int kEach = (kBins - 2 + kThreads - 1) / kThreads;  // bins of a thread, from the top
-  const int highest = kBins - 2 - (int)threadIdx.x * kEach;
+  const int highest = kBins - 2 - (int)threadIdx.x * kEach, lowest = max(highest - kEach + 1, 1);
   int kbin = 0;                             // bins below it are out by top-k
   if (known && k > 0) {
     uint32_t mine = 0, all;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (highest - i > 0) mine += count[highest - i];
+#pragma unroll 1
+    for (int i = highest; i >= lowest; --i) mine += count[i];
     uint32_t before = block_before<W>(mine, s.wave_u32, all);
     known = (uint32_t)k <= all;
     if (known) {
       if (before < (uint32_t)k && (uint32_t)k <= before + mine) {
+        int i = highest;
 #pragma unroll 1
-        for (int i = 0; i < kEach; ++i) {
-          const uint32_t c = highest - i > 0 ? count[highest - i] : 0;
-          if (before + c >= (uint32_t)k) {
-            s.found_bin = (uint32_t)(highest - i);
-            s.above_count = before;
-            break;
-          }
+        for (;; --i) {
+          const uint32_t c = count[i];
+          if (before + c >= (uint32_t)k || i <= lowest) break;
           before += c;
         }
+        s.found_bin = (uint32_t)i;
+        s.above_count = before;
       }
       __syncthreads();
       kbin = (int)s.found_bin;
@@ -647,17 +667,21 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
         known = collect_members<DT, W>(r, kbin, blocks, nblocks, members, s);
         if (known) {
           const uint32_t n = s.nmembers;
+#pragma unroll 1
           for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
             uint32_t above = 0, level = 0;
+#pragma unroll 1
             for (uint32_t j = 0; j < n; ++j) above += members[j] > members[i], level += members[j] == members[i];
             if (above < rank && rank <= above + level) s.cut_key = __builtin_bit_cast(uint32_t, members[i]);
           }
           if (threadIdx.x == 0) s.kept_mass = 0;
           __syncthreads();
           cut = __builtin_bit_cast(float, s.cut_key);
-          if (p > 0.0f)
+          if (p > 0.0f) {
+#pragma unroll 1
             for (uint32_t i = threadIdx.x; i < n; i += kThreads)
               if (members[i] >= cut) atomicAdd(&s.kept_mass, (u64)(r.weight(members[i]) * kFixed + 0.5));
+          }
           __syncthreads();
         }
       }
@@ -666,35 +690,41 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
   if (known && p > 0.0f) {
     double zero = 0.0;
     if constexpr (kOne) {
-      block_before<W>(next_to_0, s.wave_f64, zero);
+      block_before<W>(next_to_0, s.wave_f64[1], zero);
       zero *= exp2_f64(-r.m * r.c);
-      __syncthreads();
     }
     const bool ranked = k > 0 && !(kOne && kbin != kBinZero);  // bin kbin has been ranked for top-k
-    double w[kEach], mine = 0.0, all;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int bin = highest - i;
-      double n = 0.0;
-      if (bin > 0) n = kOne ? (double)count[bin] : (double)mass[bin] * (1.0 / kBinMass);
-      w[i] = n * r.weight(bin_number(bin));
-      if (kOne && bin == kBinZero) w[i] = zero;
-      if (bin < kbin) w[i] = 0.0;
-      if (ranked && bin == kbin) w[i] = (double)s.kept_mass * (1.0 / kFixed);
-      mine += w[i];
-    }
-    double before = block_before<W>(mine, s.wave_f64, all);
-    const double target = (double)p * all;
-    const uint32_t who = block_pick<W>(before, mine, kNoWeight, target, true, s);
-    if (threadIdx.x == who) {
-      bool done = false;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        if (done || !(w[i] > kNoWeight)) continue;
-        s.found_bin = (uint32_t)(highest - i);
-        s.rest = before;
-        before += w[i];
-        done = before >= target;
+    const auto bin_mass = [&](int bin) {
+      double n = kOne ? (double)count[bin] : (double)mass[bin] * (1.0 / kBinMass);
+      n *= r.weight(bin_number(bin));
+      if (kOne && bin == kBinZero) n = zero;
+      if (ranked && bin == kbin) n = (double)s.kept_mass * (1.0 / kFixed);
+      return bin < kbin ? 0.0 : n;
+    };
+    double mine = 0.0, before = 0.0, target = 0.0;
+    uint32_t who = threadIdx.x;
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {  // the thread's mass; then, in the thread that the target falls to, its bin
+      if (threadIdx.x == who) {
+        double upto = before;
+#pragma unroll 1
+        for (int i = highest; i >= lowest; --i) {
+          const double w = bin_mass(i);
+          if (round == 0) {
+            mine += w;
+          } else if (w > kNoWeight) {
+            s.found_bin = (uint32_t)i;
+            s.rest = upto;
+            upto += w;
+            if (upto >= target) break;
+          }
+        }
+      }
+      if (round == 0) {
+        double all;
+        before = block_before<W>(mine, s.wave_f64[0], all);
+        target = (double)p * all;
+        who = block_pick<W>(before, mine, target, true, s.picks[0]);
       }
     }
     __syncthreads();
@@ -707,114 +737,77 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
       if (known) {
         const uint32_t n = s.nmembers;
         u64* weights = (u64*)lds;           // over the bins
+        __syncthreads();
         if (threadIdx.x == 0) s.cut_key = 0xffffffffu;
+#pragma unroll 1
         for (uint32_t i = threadIdx.x; i < n; i += kThreads) weights[i] = (u64)(r.weight(members[i]) * kFixed + 0.5);
         __syncthreads();
+#pragma unroll 1
         for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
           if (members[i] < cut) continue;   // out by top-k
           u64 higher = 0;
+#pragma unroll 1
           for (uint32_t j = 0; j < n; ++j)
             if (members[j] > members[i]) higher += weights[j];
           if (higher == 0 || above + (double)higher * (1.0 / kFixed) < target) atomicMin(&s.cut_key, key_of(members[i]));
         }
         __syncthreads();
-        const uint32_t key = s.cut_key;
-        cut = __builtin_bit_cast(float, key >> 31 ? key & 0x7fffffffu : ~key);
+        cut = of_key(s.cut_key);
       }
     }
   }
-  if (!known) {
-    draw_by_keys<DT, W>(a, b, r, k, p, min_p, lds, s);
-    return;
-  }
+  if (!known) cut = cut_by_keys<DT, W>(r, k, p, lds, s);
+  const Kept keep{cut, min_p};
 
   // the blocks that reach the cut, in the order of the vocabulary, and their kept sums
   float least = cut;
   if (min_p > 0.0) {
-    const float down = (float)(log2(min_p) / r.c);
+    const float down = (float)(log_f64(min_p) / r.inv_t);
     least = fmaxf(least, top + down - 1e-5f * (fabsf(top) + fabsf(down)) - 1e-30f);
   }
-  uint32_t* visit = (uint32_t*)lds;
-  double* sums = (double*)(lds + (nblocks + 3) / 4 * 16);
-  const uint32_t range = (nblocks + kThreads - 1) / kThreads, from = threadIdx.x * range;
-  uint32_t n = 0, nvisit;
-  for (uint32_t j = from; j < min(from + range, nblocks); ++j) n += blocks[j] >= least && blocks[j] > kMaskedRow;
-  __syncthreads();
-  if (threadIdx.x == 0) s.first = 0xffffffffu, s.last = 0;
-  uint32_t at = block_before<W>(n, s.wave_u32, nvisit);
-  for (uint32_t j = from; j < min(from + range, nblocks); ++j)
-    if (blocks[j] >= least && blocks[j] > kMaskedRow) visit[at++] = j;
-  __syncthreads();
-  const auto kept = [&](float x) {
-    if (!(x >= cut) || !(x > kMaskedRow)) return 0.0;
-    const double w = r.weight(x);
-    return w >= min_p ? w : 0.0;
-  };
-  {
-    constexpr uint32_t kStep = kThreads / kBlockVecs;
-    const uint32_t sub = threadIdx.x % kBlockVecs;
-    const auto load = [&](uint32_t j) {
-      return j < nvisit ? __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min(visit[j] * kBlockVecs + sub, r.nvec - 1) * 16)) : vec_masked<DT>();
-    };
-    u32x4 cur[kAhead];
-#pragma unroll
-    for (int h = 0; h < kAhead; ++h) cur[h] = load(threadIdx.x / kBlockVecs + h * kStep);
+  if (known) {
+    uint32_t* visit = (uint32_t*)lds;
+    double* sums = (double*)(lds + (nblocks + 3) / 4 * 16);
+    const uint32_t range = (nblocks + kThreads - 1) / kThreads, from = threadIdx.x * range, to = min(from + range, nblocks);
+    uint32_t n = 0, nvisit;
 #pragma unroll 1
-    for (uint32_t j = threadIdx.x / kBlockVecs; j < nvisit; j += kAhead * kStep) {
-      u32x4 nxt[kAhead];
-#pragma unroll
-      for (int h = 0; h < kAhead; ++h) nxt[h] = load(j + (kAhead + h) * kStep);
-#pragma unroll
-      for (int h = 0; h < kAhead; ++h) {
-        const uint32_t q = j + h * kStep;
-        if (q >= nvisit) break;
+    for (uint32_t j = from; j < to; ++j) n += blocks[j] >= least && blocks[j] > kMaskedRow;
+    __syncthreads();
+    uint32_t at = block_before<W>(n, s.wave_u32, nvisit);
+    if (nvisit <= kThreads / kBlockVecs * kMostRounds) {
+#pragma unroll 1
+      for (uint32_t j = from; j < to; ++j)
+        if (blocks[j] >= least && blocks[j] > kMaskedRow) visit[at++] = j;
+      __syncthreads();
+      const uint32_t sub = threadIdx.x % kBlockVecs;
+#pragma unroll 1
+      for (uint32_t q = threadIdx.x / kBlockVecs; q < nvisit; q += kThreads / kBlockVecs) {
+        const u32x4 raw = vec_load<DT>(r.x, visit[q] * kBlockVecs + sub, r.V);
         float y[E];
-        logits_of<DT>(r, visit[q] * kBlockVecs + sub, cur[h], y);
+        vec_unpack<DT>(raw, y);
         uint32_t in = 0;                    // most vectors hold one kept logit or none
 #pragma unroll
-        for (uint32_t e = 0; e < E; ++e) in |= y[e] >= cut && y[e] > kMaskedRow ? 1u << e : 0u;
+        for (uint32_t e = 0; e < E; ++e) in |= y[e] >= least ? 1u << e : 0u;
         double w = 0.0;
-        for (; in != 0; in &= in - 1) w += kept(logit_in<DT>(cur[h], (uint32_t)__builtin_ctz(in)));
+        for (; in != 0; in &= in - 1) w += keep.weight(r, logit_in<DT>(raw, (uint32_t)__builtin_ctz(in)));
         w += dpp_f64<kDppRowShr1, 0xf>(w);
         w += dpp_f64<kDppRowShr2, 0xf>(w);
         w += dpp_f64<kDppRowShr4, 0xf>(w);
         w += dpp_f64<kDppRowShr8, 0xf>(w);
         if (sub == kBlockVecs - 1) sums[q] = w;
       }
-#pragma unroll
-      for (int h = 0; h < kAhead; ++h) cur[h] = nxt[h];
+      __syncthreads();
+      draw<DT, W>(a, b, r, keep, sums, nvisit, kBlockVecs, s, [&](uint32_t q) { return visit[q] * kBlockVecs; });
+      return;
     }
   }
-  __syncthreads();
-  // the block that the draw falls into
-  const uint32_t each = (nvisit + kThreads - 1) / kThreads, q0 = threadIdx.x * each;
-  double mine = 0.0, total;
-  for (uint32_t q = q0; q < min(q0 + each, nvisit); ++q) mine += sums[q];
-  const double before = block_before<W>(mine, s.wave_f64, total);
-  const double target = (double)a.u[b] * total;
-  const uint32_t who = block_pick<W>(before, mine, kNoWeight, target, false, s);
-  if (threadIdx.x == who) {
-    double rest = target - before, left = rest;
-    uint32_t q = q0;
-    for (uint32_t i = q0; i < min(q0 + each, nvisit); ++i) {
-      if (!(sums[i] > kNoWeight)) continue;
-      q = i, left = rest;
-      if (sums[i] > rest) break;
-      rest -= sums[i];
-    }
-    s.found_bin = visit[q];
-    s.rest = left;
-  }
-  __syncthreads();
-  if (wave != 0) return;
-  draw_in_vectors<DT>(a, b, r, s.found_bin * kBlockVecs + lane, lane < kBlockVecs, s.rest, total, kept);
+  draw_many<DT, W>(a, b, r, keep, lds, s);
 }
 
 template <int DT, int W, bool kFilters>
 __global__ __launch_bounds__(W* kWave) void espo_sample_kernel(SampleArgs a) {
   __shared__ SampleShared<W> s;
   extern __shared__ __align__(16) unsigned char lds[];
-  constexpr uint32_t E = vec_elems<DT>();
   const int64_t b = blockIdx.x;
   if (a.alive && !a.alive[b]) {
     if (threadIdx.x == 0) store_result(a, b, -1, 0.0f);
@@ -822,8 +815,7 @@ __global__ __launch_bounds__(W* kWave) void espo_sample_kernel(SampleArgs a) {
   }
   // beyond 1e25 the distribution is flat, and masked logits still are 10^5 times T below any other
   const float T = a.temperature ? fminf(a.temperature[b], 1e25f) : 1.0f;
-  const uint32_t nvec = (a.V + E - 1) / E;
-  Row r{a.logits + b * a.row_bytes, a.V, nvec, (nvec + kWave - 1) / kWave, 1.4426950408889634 / (double)T, 1.0 / (double)T, 0.0};
+  Row r{row_view<DT>(a.logits + b * a.row_bytes, a.V), 1.4426950408889634 / (double)T, 1.0 / (double)T, 0.0};
   if (!(T > 0.0f)) {
     greedy<DT, W>(a, b, r, s);
     return;
@@ -839,16 +831,23 @@ __global__ __launch_bounds__(W* kWave) void espo_sample_kernel(SampleArgs a) {
       return;
     }
   }
-  draw_plain<DT, W>(a, b, r, s);
+  draw_plain<DT, W>(a, b, r, lds, s);
 }
 
-// Dynamic LDS of a filtered draw: bins, then (over them) the blocks that are visited and their sums; the blocks' maxima; members.
+// Dynamic LDS of a draw without filters: the chunks' sums and references.
+template <int DT>
+size_t plain_lds(int64_t V) {
+  const size_t tile = kWave * vec_elems<DT>(), chunks = (V + tile * kChunk - 1) / (tile * kChunk);
+  return (chunks * 12 + 15) / 16 * 16;
+}
+
+// Of a filtered one: bins, then (over them) the blocks that are visited and their sums, or the chunks' sums; the blocks' maxima; members.
 template <int DT>
 size_t filter_lds(int64_t V, uint32_t& blocks, uint32_t& members) {
-  const size_t E = DT == ESPO_BF16 ? 8 : 4, ntiles = (V + kWave * E - 1) / (kWave * E), nblocks = ntiles * (kWave / kBlockVecs);
-  size_t bins = (size_t)(kBins + 3) / 4 * 16 + (DT == ESPO_BF16 ? 0 : (size_t)kBins * 8), visited = (nblocks + 3) / 4 * 16 + nblocks * 8;
-  size_t first = bins > visited ? bins : visited;
-  if (first < (size_t)kLevelBins * 12) first = (size_t)kLevelBins * 12;
+  const size_t E = vec_elems<DT>(), ntiles = (V + kWave * E - 1) / (kWave * E), nblocks = ntiles * (kWave / kBlockVecs);
+  const size_t bins = (size_t)(kBins + 3) / 4 * 16 + (DT == ESPO_BF16 ? 0 : (size_t)kBins * 8), visited = (nblocks + 3) / 4 * 16 + nblocks * 8;
+  size_t first = (size_t)kLevelBins * 12;
+  for (size_t n : {bins, visited, plain_lds<DT>(V)}) first = n > first ? n : first;
   first = (first + 15) / 16 * 16;
   blocks = (uint32_t)first;
   members = (uint32_t)(first + (nblocks + 3) / 4 * 16);
@@ -861,7 +860,7 @@ void launch(SampleArgs& a, int64_t B, hipStream_t stream) {
     const size_t lds = filter_lds<DT>(a.V, a.lds_blocks, a.lds_members);
     hipLaunchKernelGGL((espo_sample_kernel<DT, W, true>), dim3((unsigned)B), dim3(W * kWave), lds, stream, a);
   } else {
-    hipLaunchKernelGGL((espo_sample_kernel<DT, W, false>), dim3((unsigned)B), dim3(W * kWave), 0, stream, a);
+    hipLaunchKernelGGL((espo_sample_kernel<DT, W, false>), dim3((unsigned)B), dim3(W * kWave), plain_lds<DT>(a.V), stream, a);
   }
 }
 
