@@ -120,7 +120,7 @@ __device__ __forceinline__ float of_key(uint32_t key) { return __builtin_bit_cas
 
 constexpr int kLevelBins = 2048;            // of a level of the search over whole keys: 11, 11 and 10 bits
 constexpr int kMostMembers = 512;           // of a bin that are ranked, each against all others
-constexpr uint32_t kMostRounds = 4;         // of the workgroup over the blocks that are visited; beyond that the row is streamed again
+constexpr uint32_t kMostRounds = 8;         // of the workgroup over the blocks that are visited; beyond that the row is streamed again
 
 template <int W>
 struct SampleShared {
@@ -420,18 +420,19 @@ __device__ __forceinline__ void greedy(const SampleArgs& a, int64_t b, const Row
   if (lane == 0) store_result(a, b, all > kMaskedRow ? (int32_t)at : -1, 0.0f);
 }
 
-// Chunks of a row: kChunk tiles each, a wave takes every W-th.  Calls use(t, raw) for a chunk's tiles and done(chunk) after them.
-template <int W, typename Use, typename Done>
-__device__ __forceinline__ void stream_chunks(const RowView& r, Use&& use, Done&& done) {
+// Chunks of a row: kChunk tiles each, a wave takes every W-th.  Calls use(t, raw) for a chunk's tiles and done(chunk) after them, and
+// first, for the wave's first tile (the last chunk's where a wave has none), ready(t, raw); false of it ends the pass.
+template <int W, typename Ready, typename Use, typename Done>
+__device__ __forceinline__ void stream_chunks(const RowView& r, Ready&& ready, Use&& use, Done&& done) {
   const uint32_t lane = threadIdx.x & (kWave - 1), chunks = (r.ntiles + kChunk - 1) / kChunk;
   const auto load = [&](uint32_t c, uint32_t j) {
     return __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min((min(c, chunks - 1) * kChunk + j) * kWave + lane, r.nvec - 1) * 16));
   };
   uint32_t c = threadIdx.x >> 6;
-  if (c >= chunks) return;
   u32x4 cur[kChunk], nxt[kChunk];
 #pragma unroll
   for (uint32_t j = 0; j < kChunk; ++j) cur[j] = load(c, j);
+  if (!ready(min(c, chunks - 1) * kChunk, cur[0])) return;
 #pragma unroll 1
   for (; c < chunks; c += W) {
 #pragma unroll
@@ -445,72 +446,151 @@ __device__ __forceinline__ void stream_chunks(const RowView& r, Use&& use, Done&
   }
 }
 
-// No filter: the sum of every chunk, relative to a reference that follows the wave's largest logit only when that runs 2^500 ahead.
-template <int DT, int W>
-__device__ __forceinline__ void draw_plain(const SampleArgs& a, int64_t b, Row& r, unsigned char* lds, SampleShared<W>& s) {
-  constexpr uint32_t E = vec_elems<DT>(), kThreads = W * kWave;
-  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
-  double* sums = (double*)lds;
-  float* refs = (float*)(sums + chunks);
-  float m = kMaskedRow, ref = kMaskedRow, limit = kMaskedRow;
+// The kept sum of every chunk of bf16 logits, with weights from a table of all bins: 2^((x - base) c), 0 of what is not kept.  A look-up takes
+// less than half the time of a power of 2 in double (B = 512, V = 152064: 62 -> 46 us).  Logits next to 0, of which one bin
+// holds many, are weighed one by one; the two bins at the ends, of all beyond 128, count as nothing, and the caller sees to it that they may.
+// Weights are relative to r.m, the row's largest logit, or if that is not known (`find`) to the largest one of the waves' first tiles, which
+// r.m then becomes: any logit near the top does.  Returns the thread's largest logit, +inf if the table's numbers would be too large.
+template <int W>
+__device__ __forceinline__ float sum_by_table(Row& r, const Kept& keep, bool find, unsigned char* lds, double* sums, SampleShared<W>& s) {
+  constexpr uint32_t E = vec_elems<ESPO_BF16>();
+  double* table = (double*)lds;
+  const auto weight = [&](float x) {
+    const double w = r.weight(x);
+    return x >= keep.cut && w >= keep.min_p ? w : 0.0;
+  };
+  float m = kMaskedRow;
   double sum = 0.0;
-  const float lead = (float)(500.0 / r.c);
   stream_chunks<W>(
       r,
       [&](uint32_t t, u32x4 raw) {
-        float y[E];
-        tile_logits<DT>(r, t, raw, y);
-        const float top = max_of<E>(y);
-        m = fmaxf(m, top);
-        if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
-          const float to = wave_max(m);
-          sum = limit > kMaskedRow ? sum * exp2_f64(((double)ref - (double)to) * r.c) : 0.0;
-          ref = to;
-          limit = to + lead;
+        if (find) {
+          float y[E];
+          tile_logits<ESPO_BF16>(r, t, raw, y);
+          const float top = block_max<W>(max_of<E>(y), s);
+          r.m = top > kMaskedRow ? (double)top : 0.0;
+          if (!(((double)kBinsBelow - r.m) * r.c < 1000.0)) {
+            m = __builtin_huge_valf();
+            return false;
+          }
         }
-#pragma unroll
-        for (uint32_t j = 0; j < E; ++j) sum += exp2_f64(((double)y[j] - (double)ref) * r.c);
-      },
-      [&](uint32_t c) {
-        sum = wave_sum_f64(sum);
-        if (threadIdx.x % kWave == 0) sums[c] = sum, refs[c] = ref;
-        sum = 0.0;
-      });
-  const float top = block_max<W>(m, s);
-  if (!(top > kMaskedRow)) {
-    if (threadIdx.x == 0) store_result(a, b, -1, 0.0f);
-    return;
-  }
-  r.m = (double)top;
 #pragma unroll 1
-  for (uint32_t c = threadIdx.x; c < chunks; c += kThreads) sums[c] = refs[c] > kMaskedRow ? sums[c] * exp2_f64(((double)refs[c] - r.m) * r.c) : 0.0;
-  __syncthreads();
-  draw<DT, W>(a, b, r, Kept{-3.402823466e38f, 0.0}, sums, chunks, kChunk * kWave, s, [](uint32_t q) { return q * (kChunk * kWave); });
-}
-
-// Of many kept logits: the kept sum of every chunk, with the cut and the largest logit known.
-template <int DT, int W>
-__device__ __forceinline__ void draw_many(const SampleArgs& a, int64_t b, const Row& r, const Kept& keep, unsigned char* lds, SampleShared<W>& s) {
-  constexpr uint32_t E = vec_elems<DT>();
-  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
-  double* sums = (double*)lds;
-  double sum = 0.0;
-  __syncthreads();                          // what was in LDS has been read
-  stream_chunks<W>(
-      r,
+        for (int i = threadIdx.x; i < kBins; i += W * kWave) table[i] = i > 1 && i < kBins - 2 && i != kBinZero ? weight(bin_number(i)) : 0.0;
+        __syncthreads();
+        return true;
+      },
       [&](uint32_t t, u32x4 raw) {
         float y[E];
-        tile_logits<DT>(r, t, raw, y);
-        uint32_t in = 0;
+        tile_logits<ESPO_BF16>(r, t, raw, y);
+        if (t + 1 >= r.ntiles) raw = vec_pack<ESPO_BF16>(y);
+        m = fmaxf(m, max_of<E>(y));
+        float least = fabsf(y[0]);
 #pragma unroll
-        for (uint32_t e = 0; e < E; ++e) in |= y[e] >= keep.cut && y[e] > kMaskedRow ? 1u << e : 0u;
-        for (; in != 0; in &= in - 1) sum += keep.weight(r, logit_in<DT>(raw, (uint32_t)__builtin_ctz(in)));
+        for (uint32_t j = 1; j < E; ++j) least = fminf(least, fabsf(y[j]));
+        double w[E];
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+          const uint32_t at = bins_of_pair<8>(raw[j]);
+          w[2 * j] = *(const double*)(lds + (at & 0xffffu));
+          w[2 * j + 1] = *(const double*)(lds + (at >> 16));
+        }
+        sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        if (__builtin_amdgcn_ballot_w64(least < 0x1p-10f) != 0) {
+#pragma unroll 1
+          for (uint32_t j = 0; j < E; ++j) {
+            const float x = logit_in<ESPO_BF16>(raw, j);
+            if (fabsf(x) < 0x1p-10f) sum += weight(x);
+          }
+        }
       },
       [&](uint32_t c) {
         sum = wave_sum_f64(sum);
         if (threadIdx.x % kWave == 0) sums[c] = sum;
         sum = 0.0;
       });
+  return m;
+}
+
+// The same with a power of 2 for every logit.  Without a filter the largest logit is not known before: the sums are then
+// relative to a reference that follows the wave's largest logit only when that runs 2^500 ahead, and `refs` takes what each is relative to.
+template <int DT, int W, bool kFiltered>
+__device__ __forceinline__ float sum_by_powers(const Row& r, const Kept& keep, double* sums, float* refs) {
+  constexpr uint32_t E = vec_elems<DT>();
+  float m = kMaskedRow, ref = kFiltered ? (float)r.m : kMaskedRow, limit = kMaskedRow;
+  double sum = 0.0;
+  const float lead = (float)(500.0 / r.c);
+  stream_chunks<W>(
+      r, [](uint32_t, u32x4) { return true; },
+      [&](uint32_t t, u32x4 raw) {
+        float y[E];
+        tile_logits<DT>(r, t, raw, y);
+        if constexpr (!kFiltered) {
+          const float top = max_of<E>(y);
+          m = fmaxf(m, top);
+          if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
+            const float to = wave_max(m);
+            sum = limit > kMaskedRow ? sum * exp2_f64(((double)ref - (double)to) * r.c) : 0.0;
+            ref = to;
+            limit = to + lead;
+          }
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < E; ++j) {
+          const double w = exp2_f64(((double)y[j] - (double)ref) * r.c);
+          if (!kFiltered || (y[j] >= keep.cut && y[j] > kMaskedRow && w >= keep.min_p)) sum += w;
+        }
+      },
+      [&](uint32_t c) {
+        sum = wave_sum_f64(sum);
+        if (threadIdx.x % kWave == 0) {
+          sums[c] = sum;
+          if (!kFiltered) refs[c] = ref;
+        }
+        sum = 0.0;
+      });
+  return m;
+}
+
+constexpr size_t kTableBytes = (size_t)(kBins + 1) / 2 * 16;
+
+template <int DT, int W>
+__device__ __forceinline__ void draw_plain(const SampleArgs& a, int64_t b, Row& r, unsigned char* lds, SampleShared<W>& s) {
+  constexpr uint32_t kThreads = W * kWave;
+  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
+  const Kept all{-3.402823466e38f, 0.0};
+  double* sums = (double*)(lds + (DT == ESPO_BF16 ? kTableBytes : 0));
+  float* refs = (float*)(sums + chunks);
+  float top;
+  bool done = false;
+  if constexpr (DT == ESPO_BF16) {
+    top = block_max<W>(sum_by_table<W>(r, all, true, lds, sums, s), s);
+    done = !(top > kMaskedRow) || (top < kBinsBelow && ((double)top + kBinsBelow) * r.inv_t > 50.0);
+    __syncthreads();
+  }
+  if (!done) {
+    top = block_max<W>(sum_by_powers<DT, W, false>(r, all, sums, refs), s);
+    r.m = (double)top;
+#pragma unroll 1
+    for (uint32_t c = threadIdx.x; c < chunks; c += kThreads) sums[c] = refs[c] > kMaskedRow ? sums[c] * exp2_f64(((double)refs[c] - r.m) * r.c) : 0.0;
+    __syncthreads();
+  }
+  if (!(top > kMaskedRow)) {
+    if (threadIdx.x == 0) store_result(a, b, -1, 0.0f);
+    return;
+  }
+  draw<DT, W>(a, b, r, all, sums, chunks, kChunk * kWave, s, [](uint32_t q) { return q * (kChunk * kWave); });
+}
+
+// Of many kept logits: the kept sum of every chunk, with the cut and the largest logit known.
+template <int DT, int W>
+__device__ __forceinline__ void draw_many(const SampleArgs& a, int64_t b, Row& r, const Kept& keep, unsigned char* lds, SampleShared<W>& s) {
+  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
+  double* sums = (double*)(lds + (DT == ESPO_BF16 ? kTableBytes : 0));
+  __syncthreads();                          // what was in LDS has been read
+  if (DT == ESPO_BF16 && r.m < (double)kBinsBelow && keep.cut > -kBinsBelow)
+    sum_by_table<W>(r, keep, false, lds, sums, s);
+  else
+    sum_by_powers<DT, W, true>(r, keep, sums, nullptr);
   __syncthreads();
   draw<DT, W>(a, b, r, keep, sums, chunks, kChunk * kWave, s, [](uint32_t q) { return q * (kChunk * kWave); });
 }
@@ -709,6 +789,7 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
         double upto = before;
 #pragma unroll 1
         for (int i = highest; i >= lowest; --i) {
+          if (kOne && __builtin_amdgcn_ballot_w64(count[i] != 0) == 0) continue;
           const double w = bin_mass(i);
           if (round == 0) {
             mine += w;
@@ -834,11 +915,11 @@ __global__ __launch_bounds__(W* kWave) void espo_sample_kernel(SampleArgs a) {
   draw_plain<DT, W>(a, b, r, lds, s);
 }
 
-// Dynamic LDS of a draw without filters: the chunks' sums and references.
+// Dynamic LDS of a draw without filters: the weights of all bins, the chunks' sums and references.
 template <int DT>
 size_t plain_lds(int64_t V) {
   const size_t tile = kWave * vec_elems<DT>(), chunks = (V + tile * kChunk - 1) / (tile * kChunk);
-  return (chunks * 12 + 15) / 16 * 16;
+  return (DT == ESPO_BF16 ? kTableBytes : 0) + (chunks * 12 + 15) / 16 * 16;
 }
 
 // Of a filtered one: bins, then (over them) the blocks that are visited and their sums, or the chunks' sums; the blocks' maxima; members.
