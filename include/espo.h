@@ -512,6 +512,10 @@ int espo_length_order(const int32_t* lengths, int64_t B, int64_t T, int32_t* ord
  *   alive       device, [B] uint8, or NULL: every row is live.
  *   tokens      device, [B] int32 out.
  *   logprob     device, [B] fp32 out, may be NULL.
+ *   workspace   optional device scratch of at least espo_sample_workspace_bytes(B, V, dt) bytes, 16-byte aligned.  With it, the rows of a
+ *               small batch are split over several workgroups.  Without it (NULL, too short or misaligned), and where that size is 0, one
+ *               workgroup handles a whole row.  What it holds before and after the call does not matter; calls that may run
+ *               at the same time need a workspace each.
  *   stream      hipStream_t as void*.
  */
 int espo_sample(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_t row_stride, const float* temperature,

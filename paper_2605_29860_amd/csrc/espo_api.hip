@@ -393,14 +393,13 @@ int espo_advantages_packed(const float* rewards, const float* terminal_reward, c
 }
 
 size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt) {
-  (void)B; (void)V; (void)dt;
-  return 0;
+  if (B <= 0 || V < 1 || V > (1 << 20) || (dt != ESPO_F32 && dt != ESPO_BF16)) return 0;
+  return espo::sample_workspace(dt, B, V);
 }
 
 int espo_sample(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_t row_stride, const float* temperature,
                 const int32_t* top_k, const float* top_p, const float* min_p, const float* u, const uint8_t* alive, int32_t* tokens,
                 float* logprob, void* workspace, size_t workspace_bytes, void* stream) {
-  (void)workspace; (void)workspace_bytes;
   if (dt != ESPO_F32 && dt != ESPO_BF16) return ESPO_EINVAL;
   if (B < 0 || V < 1 || row_stride < V) return ESPO_EINVAL;
   if (B == 0) return ESPO_OK;
@@ -408,7 +407,7 @@ int espo_sample(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_t
   if (B > 0x7fffffff || V > (top_k || top_p || min_p ? 1 << 19 : 1 << 20)) return ESPO_ERANGE;  // a filter keeps the maxima of blocks in LDS
   if (!aligned16(logits) || ((size_t)row_stride * (dt == ESPO_BF16 ? 2 : 4)) % 16 != 0) return ESPO_EALIGN;
   return espo::launch_sample(logits, dt, B, V, row_stride, temperature, top_k, top_p, min_p, u, alive, tokens, logprob,
-                             (hipStream_t)stream);
+                             workspace, workspace_bytes, (hipStream_t)stream);
 }
 
 size_t espo_logprobs_workspace_bytes(int64_t N, int64_t V, espo_dtype dt) {

@@ -80,7 +80,9 @@ int launch_length_order(const int32_t* lengths, int64_t B, int64_t T, int32_t* o
 
 int launch_sample(const void* logits, int dt, int64_t B, int64_t V, int64_t row_stride, const float* temperature, const int32_t* top_k,
                   const float* top_p, const float* min_p, const float* u, const uint8_t* alive, int32_t* tokens, float* logprob,
-                  hipStream_t stream);
+                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+// Bytes with which the rows of a small batch are split over several workgroups, 0 where they are not.
+size_t sample_workspace(int dt, int64_t B, int64_t V);
 
 // The policy update's operators.  stats: [N] pairs of row maximum and sum.
 int launch_logprobs(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,

@@ -43,6 +43,7 @@ constexpr int kMagSpan = 17 << 7;                 // numbers from 2^-10 to 128
 constexpr int kBinZero = kMagSpan + 2;            // bin of everything next to 0
 constexpr int kBins = 2 * kBinZero + 1;           // the first and the last usable one, 1 and kBins - 2, stand for all beyond 128
 constexpr float kBinsBelow = 128.0f;
+constexpr size_t kCountBytes = (size_t)(kBins + 3) / 4 * 16;
 constexpr double kBinMass = 1099511627776.0;      // 2^40: the mass of a bin is in units of 2^-40 of its own number's weight
 
 __device__ __forceinline__ int bin_of(uint32_t bits) {
@@ -93,6 +94,26 @@ __device__ __forceinline__ double exp2_f64(double t) {
   return __hiloint2double(__double2hiint(q) + (int)((uint32_t)__double2loint(z) << 20), __double2loint(q));
 }
 
+// The integer nearest to w * scale, which is below 2^51: the low bits of the sum with 2^52.
+__device__ __forceinline__ unsigned long long fixed_point(double w, double scale) {
+  return __builtin_bit_cast(unsigned long long, fma(w, scale, 4503599627370496.0)) - 0x4330000000000000ull;
+}
+
+// What the workgroups of a split row leave for its draw: its blocks' maxima (or, without a filter, its chunks' sums and references), and
+// of each workgroup its largest logit, its mass next to 0 and its bins.
+struct PartRecord {
+  double next_to_0;
+  float m, pad;
+};
+struct SplitLayout {
+  char* base;
+  size_t row, bins;  // bytes of a row, of a workgroup's bins
+  uint32_t parts, front;
+  __device__ __forceinline__ char* of(int64_t b) const { return base + (size_t)b * row; }
+  __device__ __forceinline__ PartRecord* records(int64_t b) const { return (PartRecord*)(of(b) + front); }
+  __device__ __forceinline__ char* part_bins(int64_t b, uint32_t part) const { return of(b) + front + parts * sizeof(PartRecord) + part * bins; }
+};
+
 struct SampleArgs {
   const char* logits;
   int64_t row_bytes;
@@ -104,6 +125,7 @@ struct SampleArgs {
   int32_t* tokens;
   float* logprob;
   uint32_t lds_blocks, lds_members;  // where the blocks' maxima and a bin's members start in dynamic LDS
+  SplitLayout split;
 };
 
 struct Row : RowView {
@@ -119,7 +141,8 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float of_key(uint32_t key) { return __builtin_bit_cast(float, key >> 31 ? key & 0x7fffffffu : ~key); }
 
 constexpr int kLevelBins = 2048;            // of a level of the search over whole keys: 11, 11 and 10 bits
-constexpr int kMostMembers = 512;           // of a bin that are ranked, each against all others
+constexpr int kMostMembers = 512;           // logits of a bin that are ranked, each against all others
+constexpr int kMostFew = 400;               // top-k up to this ranks the k largest of fp32 logits, with their bin's others
 constexpr uint32_t kMostRounds = 8;         // of the workgroup over the blocks that are visited; beyond that the row is streamed again
 
 template <int W>
@@ -273,7 +296,7 @@ __device__ __forceinline__ uint32_t find_cut(const Row& r, uint32_t floor, const
         if (!(x > kMaskedRow) || key < floor || (level > 0 && (key >> (shift + bits)) != prefix)) continue;
         const uint32_t bin = (key >> shift) & ((1u << bits) - 1);
         atomicAdd(&count[bin], 1u);
-        atomicAdd(&mass[bin], (u64)(r.weight(x) * kFixed + 0.5));
+        atomicAdd(&mass[bin], fixed_point(r.weight(x), kFixed));
       }
     }
     __syncthreads();
@@ -420,21 +443,21 @@ __device__ __forceinline__ void greedy(const SampleArgs& a, int64_t b, const Row
   if (lane == 0) store_result(a, b, all > kMaskedRow ? (int32_t)at : -1, 0.0f);
 }
 
-// Chunks of a row: kChunk tiles each, a wave takes every W-th.  Calls use(t, raw) for a chunk's tiles and done(chunk) after them, and
+// Chunks c0 .. c1 - 1 of a row: kChunk tiles each, a wave takes every W-th.  Calls use(t, raw) for a chunk's tiles and done(chunk) after them, and
 // first, for the wave's first tile (the last chunk's where a wave has none), ready(t, raw); false of it ends the pass.
 template <int W, typename Ready, typename Use, typename Done>
-__device__ __forceinline__ void stream_chunks(const RowView& r, Ready&& ready, Use&& use, Done&& done) {
-  const uint32_t lane = threadIdx.x & (kWave - 1), chunks = (r.ntiles + kChunk - 1) / kChunk;
+__device__ __forceinline__ void stream_chunks(const RowView& r, uint32_t c0, uint32_t c1, Ready&& ready, Use&& use, Done&& done) {
+  const uint32_t lane = threadIdx.x & (kWave - 1);
   const auto load = [&](uint32_t c, uint32_t j) {
-    return __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min((min(c, chunks - 1) * kChunk + j) * kWave + lane, r.nvec - 1) * 16));
+    return __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min((min(c, c1 - 1) * kChunk + j) * kWave + lane, r.nvec - 1) * 16));
   };
-  uint32_t c = threadIdx.x >> 6;
+  uint32_t c = c0 + (threadIdx.x >> 6);
   u32x4 cur[kChunk], nxt[kChunk];
 #pragma unroll
   for (uint32_t j = 0; j < kChunk; ++j) cur[j] = load(c, j);
-  if (!ready(min(c, chunks - 1) * kChunk, cur[0])) return;
+  if (!ready(min(c, c1 - 1) * kChunk, cur[0])) return;
 #pragma unroll 1
-  for (; c < chunks; c += W) {
+  for (; c < c1; c += W) {
 #pragma unroll
     for (uint32_t j = 0; j < kChunk; ++j) nxt[j] = load(c + W, j);
 #pragma unroll
@@ -452,7 +475,7 @@ __device__ __forceinline__ void stream_chunks(const RowView& r, Ready&& ready, U
 // Weights are relative to r.m, the row's largest logit, or if that is not known (`find`) to the largest one of the waves' first tiles, which
 // r.m then becomes: any logit near the top does.  Returns the thread's largest logit, +inf if the table's numbers would be too large.
 template <int W>
-__device__ __forceinline__ float sum_by_table(Row& r, const Kept& keep, bool find, unsigned char* lds, double* sums, SampleShared<W>& s) {
+__device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, const Kept& keep, bool find, unsigned char* lds, double* sums, SampleShared<W>& s) {
   constexpr uint32_t E = vec_elems<ESPO_BF16>();
   double* table = (double*)lds;
   const auto weight = [&](float x) {
@@ -462,7 +485,7 @@ __device__ __forceinline__ float sum_by_table(Row& r, const Kept& keep, bool fin
   float m = kMaskedRow;
   double sum = 0.0;
   stream_chunks<W>(
-      r,
+      r, c0, c1,
       [&](uint32_t t, u32x4 raw) {
         if (find) {
           float y[E];
@@ -514,13 +537,13 @@ __device__ __forceinline__ float sum_by_table(Row& r, const Kept& keep, bool fin
 // The same with a power of 2 for every logit.  Without a filter the largest logit is not known before: the sums are then
 // relative to a reference that follows the wave's largest logit only when that runs 2^500 ahead, and `refs` takes what each is relative to.
 template <int DT, int W, bool kFiltered>
-__device__ __forceinline__ float sum_by_powers(const Row& r, const Kept& keep, double* sums, float* refs) {
+__device__ __forceinline__ float sum_by_powers(const Row& r, uint32_t c0, uint32_t c1, const Kept& keep, double* sums, float* refs) {
   constexpr uint32_t E = vec_elems<DT>();
   float m = kMaskedRow, ref = kFiltered ? (float)r.m : kMaskedRow, limit = kMaskedRow;
   double sum = 0.0;
   const float lead = (float)(500.0 / r.c);
   stream_chunks<W>(
-      r, [](uint32_t, u32x4) { return true; },
+      r, c0, c1, [](uint32_t, u32x4) { return true; },
       [&](uint32_t t, u32x4 raw) {
         float y[E];
         tile_logits<DT>(r, t, raw, y);
@@ -553,32 +576,36 @@ __device__ __forceinline__ float sum_by_powers(const Row& r, const Kept& keep, d
 
 constexpr size_t kTableBytes = (size_t)(kBins + 1) / 2 * 16;
 
+// No filter: the sums of chunks c0 .. c1 - 1 (sums[0] is chunk 0's), and what each is relative to.  Returns the largest logit.
 template <int DT, int W>
-__device__ __forceinline__ void draw_plain(const SampleArgs& a, int64_t b, Row& r, unsigned char* lds, SampleShared<W>& s) {
-  constexpr uint32_t kThreads = W * kWave;
-  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
+__device__ __forceinline__ float sum_plain(Row& r, uint32_t c0, uint32_t c1, unsigned char* lds, double* sums, float* refs, SampleShared<W>& s) {
   const Kept all{-3.402823466e38f, 0.0};
-  double* sums = (double*)(lds + (DT == ESPO_BF16 ? kTableBytes : 0));
-  float* refs = (float*)(sums + chunks);
-  float top;
-  bool done = false;
   if constexpr (DT == ESPO_BF16) {
-    top = block_max<W>(sum_by_table<W>(r, all, true, lds, sums, s), s);
-    done = !(top > kMaskedRow) || (top < kBinsBelow && ((double)top + kBinsBelow) * r.inv_t > 50.0);
+    const float top = block_max<W>(sum_by_table<W>(r, c0, c1, all, true, lds, sums, s), s);
     __syncthreads();
-  }
-  if (!done) {
-    top = block_max<W>(sum_by_powers<DT, W, false>(r, all, sums, refs), s);
-    r.m = (double)top;
+    if (!(top > kMaskedRow) || (top < kBinsBelow && ((double)top + kBinsBelow) * r.inv_t > 50.0)) {
 #pragma unroll 1
-    for (uint32_t c = threadIdx.x; c < chunks; c += kThreads) sums[c] = refs[c] > kMaskedRow ? sums[c] * exp2_f64(((double)refs[c] - r.m) * r.c) : 0.0;
-    __syncthreads();
+      for (uint32_t c = c0 + threadIdx.x; c < c1; c += W * kWave) refs[c] = top > kMaskedRow ? (float)r.m : kMaskedRow;
+      return top;
+    }
   }
+  return block_max<W>(sum_by_powers<DT, W, false>(r, c0, c1, all, sums, refs), s);
+}
+
+// Its draw, once the largest logit is known and the sums are in LDS.
+template <int DT, int W>
+__device__ __forceinline__ void draw_plain(const SampleArgs& a, int64_t b, Row& r, float top, double* sums, const float* refs, SampleShared<W>& s) {
+  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
   if (!(top > kMaskedRow)) {
     if (threadIdx.x == 0) store_result(a, b, -1, 0.0f);
     return;
   }
-  draw<DT, W>(a, b, r, all, sums, chunks, kChunk * kWave, s, [](uint32_t q) { return q * (kChunk * kWave); });
+  r.m = (double)top;
+  __syncthreads();
+#pragma unroll 1
+  for (uint32_t c = threadIdx.x; c < chunks; c += W * kWave) sums[c] = refs[c] > kMaskedRow ? sums[c] * exp2_f64(((double)refs[c] - r.m) * r.c) : 0.0;
+  __syncthreads();
+  draw<DT, W>(a, b, r, Kept{-3.402823466e38f, 0.0}, sums, chunks, kChunk * kWave, s, [](uint32_t q) { return q * (kChunk * kWave); });
 }
 
 // Of many kept logits: the kept sum of every chunk, with the cut and the largest logit known.
@@ -588,9 +615,9 @@ __device__ __forceinline__ void draw_many(const SampleArgs& a, int64_t b, Row& r
   double* sums = (double*)(lds + (DT == ESPO_BF16 ? kTableBytes : 0));
   __syncthreads();                          // what was in LDS has been read
   if (DT == ESPO_BF16 && r.m < (double)kBinsBelow && keep.cut > -kBinsBelow)
-    sum_by_table<W>(r, keep, false, lds, sums, s);
+    sum_by_table<W>(r, 0, chunks, keep, false, lds, sums, s);
   else
-    sum_by_powers<DT, W, true>(r, keep, sums, nullptr);
+    sum_by_powers<DT, W, true>(r, 0, chunks, keep, sums, nullptr);
   __syncthreads();
   draw<DT, W>(a, b, r, keep, sums, chunks, kChunk * kWave, s, [](uint32_t q) { return q * (kChunk * kWave); });
 }
@@ -610,45 +637,70 @@ __device__ __forceinline__ float cut_by_keys(const Row& r, int32_t k, float p, u
   return of_key(floor);
 }
 
-// Collects the logits of one bin; false if there are more than are ranked.
+// Collects the logits of one bin, or of it and all above; false if there are more than are ranked.
 template <int DT, int W>
-__device__ __forceinline__ bool collect_members(const Row& r, int bin, const float* blocks, uint32_t nblocks, float* members, SampleShared<W>& s) {
-  constexpr uint32_t E = vec_elems<DT>();
+__device__ __forceinline__ bool collect_members(const Row& r, int bin, bool above, const float* blocks, uint32_t nblocks, float* members, SampleShared<W>& s) {
+  constexpr uint32_t E = vec_elems<DT>(), kStep = W * kWave / kBlockVecs;
   __syncthreads();
   if (threadIdx.x == 0) s.nmembers = 0;
   __syncthreads();
   const float floor = bin_floor(bin);
 #pragma unroll 1
-  for (uint32_t j = threadIdx.x / kBlockVecs; j < nblocks; j += W * kWave / kBlockVecs) {
-    if (!(blocks[j] >= floor)) continue;
-    const uint32_t i = j * kBlockVecs + threadIdx.x % kBlockVecs;
-    float y[E];
-    vec_unpack<DT>(vec_load<DT>(r.x, i, r.V), y);
+  for (uint32_t j = threadIdx.x / kBlockVecs; j < nblocks; j += kAhead * kStep) {
+    u32x4 raw[kAhead];
 #pragma unroll
-    for (uint32_t e = 0; e < E; ++e) {
-      if (!(y[e] > -kBinsBelow) || bin_of(__builtin_bit_cast(uint32_t, y[e])) != bin) continue;
+    for (int h = 0; h < kAhead; ++h) {      // those that reach the bin, all on their way at once
+      const uint32_t q = j + h * kStep;
+      raw[h] = vec_masked<DT>();
+      if (q < nblocks && blocks[q] >= floor)
+        raw[h] = __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min(q * kBlockVecs + threadIdx.x % kBlockVecs, r.nvec - 1) * 16));
+    }
+    uint32_t in = 0;
+#pragma unroll
+    for (int h = 0; h < kAhead; ++h) {
+      float y[E];
+      vec_unpack<DT>(raw[h], y);
+#pragma unroll
+      for (uint32_t e = 0; e < E; ++e) in |= y[e] >= floor ? 1u << (h * E + e) : 0u;
+    }
+    for (; in != 0; in &= in - 1) {
+      const uint32_t at_bit = (uint32_t)__builtin_ctz(in), h = at_bit / E, e = at_bit % E;
+      u32x4 v = raw[0];
+#pragma unroll
+      for (uint32_t q = 1; q < kAhead; ++q) v = h == q ? raw[q] : v;
+      const float x = logit_in<DT>(v, e);
+      const int at_bin = bin_of(__builtin_bit_cast(uint32_t, x));
+      const bool beyond = ((j + h * kStep) * kBlockVecs + threadIdx.x % kBlockVecs) * E + e >= r.V;
+      if (beyond || !(x > -kBinsBelow) || (above ? at_bin < bin : at_bin != bin)) continue;
       const uint32_t at = atomicAdd(&s.nmembers, 1u);
-      if (at < kMostMembers) members[at] = y[e];
+      if (at < kMostMembers) members[at] = x;
     }
   }
   __syncthreads();
   return s.nmembers <= kMostMembers;
 }
 
+// What the filters of a row ask for, and what a pass over it has to leave for them.
+struct Filters {
+  int32_t k;       // 0: off
+  float p;         // 0: off
+  double min_p;
+  bool few;        // fp32 logits, and so small a k that all of the k largest are ranked
+  bool counts, masses;
+};
+
+// The bins of tiles t0 .. t1 - 1, and the largest logit of each of their blocks.  Returns the thread's largest logit; next_to_0 is its share
+// of the mass of bf16 logits next to 0, relative to e^0.
 template <int DT, int W>
-__device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Row& r, int32_t k, float p, double min_p, unsigned char* lds,
-                                              SampleShared<W>& s) {
+__device__ __forceinline__ float fill_bins(const Row& r, uint32_t t0, uint32_t t1, const Filters& f, unsigned char* lds, float* blocks, double& next_to_0) {
   constexpr uint32_t E = vec_elems<DT>();
   constexpr int kThreads = W * kWave;
-  constexpr bool kOne = DT == ESPO_BF16;    // one value per bin: its mass follows from its count
+  constexpr bool kOne = DT == ESPO_BF16;
   const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
-  const uint32_t nblocks = r.ntiles * (kWave / kBlockVecs);
   uint32_t* count = (uint32_t*)lds;
-  u64* mass = (u64*)(lds + (kBins + 3) / 4 * 16);
-  float* blocks = (float*)(lds + a.lds_blocks);
-  float* members = (float*)(lds + a.lds_members);
-  const bool counts = k > 0 || (kOne && p > 0.0f), masses = !kOne && p > 0.0f;
-
+  u64* mass = (u64*)(lds + kCountBytes);
+  const bool counts = f.counts, masses = f.masses;
+  const float p = f.p;
   if (counts || masses) {
 #pragma unroll 1
     for (int i = threadIdx.x; i < kBins; i += kThreads) {
@@ -658,8 +710,7 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
     __syncthreads();
   }
   float m = kMaskedRow;
-  double next_to_0 = 0.0;                   // mass of bf16 logits next to 0, relative to e^0
-  stream_ring(r, wave, r.ntiles, W, [&](uint32_t t, u32x4 raw) {
+  stream_ring(r, t0 + wave, t1, W, [&](uint32_t t, u32x4 raw) {
     float y[E];
     tile_logits<DT>(r, t, raw, y);
     float top = max_of<E>(y);
@@ -699,10 +750,66 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
         if (!(y[j] > -kBinsBelow)) continue;
         const int bin = bin_of(__builtin_bit_cast(uint32_t, y[j]));
         const double rel = exp2_f64((double)(y[j] - bin_number(bin)) * r.c);
-        atomicAdd(&mass[bin], (u64)(rel * kBinMass + 0.5));
+        atomicAdd(&mass[bin], fixed_point(rel, kBinMass));
       }
     }
   });
+  return m;
+}
+
+// The parts' bins and blocks put together in LDS; what fill_bins leaves of a whole row.
+template <int DT, int W>
+__device__ __forceinline__ float join_parts(const SplitLayout& split, int64_t b, const Row& r, const Filters& f, unsigned char* lds, float* blocks,
+                                            double& next_to_0) {
+  constexpr int kThreads = W * kWave;
+  const uint32_t nblocks = r.ntiles * (kWave / kBlockVecs);
+  const float* from = (const float*)split.of(b);
+  const PartRecord* records = split.records(b);
+  float m = kMaskedRow;
+#pragma unroll 1
+  for (uint32_t j = threadIdx.x; j < nblocks; j += kThreads) blocks[j] = from[j];
+  if (threadIdx.x < split.parts) m = records[threadIdx.x].m, next_to_0 = records[threadIdx.x].next_to_0;
+  // The counts, and behind them the masses, as 16 bytes at a time: sums of words without a carry, and of pairs with one.
+  if (f.counts) {
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x; i < kCountBytes / 16; i += kThreads) {
+      u32x4 n{0, 0, 0, 0};
+      for (uint32_t q = 0; q < split.parts; ++q) n += ((const u32x4*)split.part_bins(b, q))[i];
+      ((u32x4*)lds)[i] = n;
+    }
+  }
+  if (f.masses) {
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x; i < kBins; i += kThreads) {
+      u64 n = 0;
+      for (uint32_t q = 0; q < split.parts; ++q) n += ((const u64*)(split.part_bins(b, q) + kCountBytes))[i];
+      ((u64*)(lds + kCountBytes))[i] = n;
+    }
+  }
+  return m;                                 // (block_max has the barrier)
+}
+
+template <int DT, int W, bool kJoin>
+__device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Row& r, const Filters& f, unsigned char* lds, SampleShared<W>& s) {
+  constexpr uint32_t E = vec_elems<DT>();
+  constexpr int kThreads = W * kWave;
+  constexpr bool kOne = DT == ESPO_BF16;    // one value per bin: its mass follows from its count
+  const int32_t k = f.k;
+  const float p = f.p;
+  const double min_p = f.min_p;
+  const bool masses = f.masses;
+  const uint32_t nblocks = r.ntiles * (kWave / kBlockVecs);
+  uint32_t* count = (uint32_t*)lds;
+  u64* mass = (u64*)(lds + kCountBytes);
+  float* blocks = (float*)(lds + a.lds_blocks);
+  float* members = (float*)(lds + a.lds_members);
+  double next_to_0 = 0.0;
+  float m = kMaskedRow;
+  if constexpr (kJoin) {
+    m = join_parts<DT, W>(a.split, b, r, f, lds, blocks, next_to_0);
+  } else {
+    m = fill_bins<DT, W>(r, 0, r.ntiles, f, lds, blocks, next_to_0);
+  }
   const float top = block_max<W>(m, s);
   if (!(top > kMaskedRow)) {
     if (threadIdx.x == 0) store_result(a, b, -1, 0.0f);
@@ -743,15 +850,16 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
       if (kOne && kbin != kBinZero) {
         cut = bin_number(kbin);
       } else {
-        const uint32_t rank = (uint32_t)k - s.above_count;  // within the bin, from 1
-        known = collect_members<DT, W>(r, kbin, blocks, nblocks, members, s);
+        const uint32_t rank = (uint32_t)k - (f.few ? 0 : s.above_count);  // among the members, from 1
+        known = collect_members<DT, W>(r, kbin, f.few, blocks, nblocks, members, s);
         if (known) {
           const uint32_t n = s.nmembers;
 #pragma unroll 1
           for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
             uint32_t above = 0, level = 0;
-#pragma unroll 1
-            for (uint32_t j = 0; j < n; ++j) above += members[j] > members[i], level += members[j] == members[i];
+            const float mine = members[i];
+#pragma unroll 8
+            for (uint32_t j = 0; j < n; ++j) above += members[j] > mine, level += members[j] == mine;
             if (above < rank && rank <= above + level) s.cut_key = __builtin_bit_cast(uint32_t, members[i]);
           }
           if (threadIdx.x == 0) s.kept_mass = 0;
@@ -760,14 +868,19 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
           if (p > 0.0f) {
 #pragma unroll 1
             for (uint32_t i = threadIdx.x; i < n; i += kThreads)
-              if (members[i] >= cut) atomicAdd(&s.kept_mass, (u64)(r.weight(members[i]) * kFixed + 0.5));
+              if (members[i] >= cut) atomicAdd(&s.kept_mass, fixed_point(r.weight(members[i]), kFixed));
           }
           __syncthreads();
         }
       }
     }
   }
-  if (known && p > 0.0f) {
+  bool rank_mass = false;                   // the nucleus ends among the members
+  double above = 0.0, target = 0.0;         // their mass from the top: what lies above them, and where the nucleus ends
+  if (known && p > 0.0f && f.few) {
+    rank_mass = true;
+    target = (double)p * (double)s.kept_mass * (1.0 / kFixed);
+  } else if (known && p > 0.0f) {
     double zero = 0.0;
     if constexpr (kOne) {
       block_before<W>(next_to_0, s.wave_f64[1], zero);
@@ -781,7 +894,7 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
       if (ranked && bin == kbin) n = (double)s.kept_mass * (1.0 / kFixed);
       return bin < kbin ? 0.0 : n;
     };
-    double mine = 0.0, before = 0.0, target = 0.0;
+    double mine = 0.0, before = 0.0;
     uint32_t who = threadIdx.x;
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {  // the thread's mass; then, in the thread that the target falls to, its bin
@@ -789,7 +902,7 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
         double upto = before;
 #pragma unroll 1
         for (int i = highest; i >= lowest; --i) {
-          if (kOne && __builtin_amdgcn_ballot_w64(count[i] != 0) == 0) continue;
+          if (__builtin_amdgcn_ballot_w64(kOne ? count[i] != 0 : mass[i] != 0) == 0) continue;
           const double w = bin_mass(i);
           if (round == 0) {
             mine += w;
@@ -810,32 +923,33 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
     }
     __syncthreads();
     const int bin = (int)s.found_bin;
-    const double above = s.rest;
+    above = s.rest;
     if (kOne && bin != kBinZero) {
       cut = bin_number(bin);
     } else {
-      if (bin != kbin || k == 0) known = collect_members<DT, W>(r, bin, blocks, nblocks, members, s);
-      if (known) {
-        const uint32_t n = s.nmembers;
-        u64* weights = (u64*)lds;           // over the bins
-        __syncthreads();
-        if (threadIdx.x == 0) s.cut_key = 0xffffffffu;
-#pragma unroll 1
-        for (uint32_t i = threadIdx.x; i < n; i += kThreads) weights[i] = (u64)(r.weight(members[i]) * kFixed + 0.5);
-        __syncthreads();
-#pragma unroll 1
-        for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-          if (members[i] < cut) continue;   // out by top-k
-          u64 higher = 0;
-#pragma unroll 1
-          for (uint32_t j = 0; j < n; ++j)
-            if (members[j] > members[i]) higher += weights[j];
-          if (higher == 0 || above + (double)higher * (1.0 / kFixed) < target) atomicMin(&s.cut_key, key_of(members[i]));
-        }
-        __syncthreads();
-        cut = of_key(s.cut_key);
-      }
+      rank_mass = true;
+      if (bin != kbin || k == 0) known = collect_members<DT, W>(r, bin, false, blocks, nblocks, members, s);
     }
+  }
+  if (known && rank_mass) {
+    const uint32_t n = s.nmembers;
+    u64* weights = (u64*)lds;               // over the bins
+    __syncthreads();
+    if (threadIdx.x == 0) s.cut_key = 0xffffffffu;
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x; i < n; i += kThreads) weights[i] = fixed_point(r.weight(members[i]), kFixed);
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+      if (members[i] < cut) continue;       // out by top-k
+      const float mine = members[i];
+      u64 higher = 0;
+#pragma unroll 8
+      for (uint32_t j = 0; j < n; ++j) higher += members[j] > mine ? weights[j] : 0;
+      if (higher == 0 || above + (double)higher * (1.0 / kFixed) < target) atomicMin(&s.cut_key, key_of(members[i]));
+    }
+    __syncthreads();
+    cut = of_key(s.cut_key);
   }
   if (!known) cut = cut_by_keys<DT, W>(r, k, p, lds, s);
   const Kept keep{cut, min_p};
@@ -885,7 +999,35 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
   draw_many<DT, W>(a, b, r, keep, lds, s);
 }
 
-template <int DT, int W, bool kFilters>
+// A row's settings.
+struct RowPlan {
+  float T;
+  Filters f;
+  __device__ __forceinline__ bool is_greedy() const { return !(T > 0.0f); }
+  __device__ __forceinline__ bool is_plain() const { return f.k == 0 && f.p == 0.0f && !(f.min_p > 0.0); }
+};
+template <int DT>
+__device__ __forceinline__ RowPlan row_plan(const SampleArgs& a, int64_t b) {
+  RowPlan w;
+  // beyond 1e25 the distribution is flat, and masked logits still are 10^5 times T below any other
+  w.T = a.temperature ? fminf(a.temperature[b], 1e25f) : 1.0f;
+  const int32_t k = a.top_k ? a.top_k[b] : 0;
+  const float p = a.top_p ? a.top_p[b] : 0.0f;
+  w.f.k = k > 0 && (uint32_t)k < a.V ? k : 0;
+  w.f.p = p > 0.0f && p < 1.0f ? p : 0.0f;
+  w.f.min_p = a.min_p ? (double)fminf(a.min_p[b], 1.0f) : 0.0;
+  w.f.counts = w.f.k > 0 || (DT == ESPO_BF16 && w.f.p > 0.0f);
+  w.f.few = DT != ESPO_BF16 && w.f.k > 0 && w.f.k <= kMostFew;
+  w.f.masses = DT != ESPO_BF16 && w.f.p > 0.0f && !w.f.few;
+  return w;
+}
+template <int DT>
+__device__ __forceinline__ Row row_of(const SampleArgs& a, int64_t b, float T) {
+  return Row{row_view<DT>(a.logits + b * a.row_bytes, a.V), 1.4426950408889634 / (double)T, 1.0 / (double)T, 0.0};
+}
+
+// kJoin: the passes over the row have been made by espo_sample_part_kernel.
+template <int DT, int W, bool kFilters, bool kJoin>
 __global__ __launch_bounds__(W* kWave) void espo_sample_kernel(SampleArgs a) {
   __shared__ SampleShared<W> s;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -894,25 +1036,75 @@ __global__ __launch_bounds__(W* kWave) void espo_sample_kernel(SampleArgs a) {
     if (threadIdx.x == 0) store_result(a, b, -1, 0.0f);
     return;
   }
-  // beyond 1e25 the distribution is flat, and masked logits still are 10^5 times T below any other
-  const float T = a.temperature ? fminf(a.temperature[b], 1e25f) : 1.0f;
-  Row r{row_view<DT>(a.logits + b * a.row_bytes, a.V), 1.4426950408889634 / (double)T, 1.0 / (double)T, 0.0};
-  if (!(T > 0.0f)) {
+  const RowPlan w = row_plan<DT>(a, b);
+  Row r = row_of<DT>(a, b, w.T);
+  if (w.is_greedy()) {
     greedy<DT, W>(a, b, r, s);
     return;
   }
   if constexpr (kFilters) {
-    int32_t k = a.top_k ? a.top_k[b] : 0;
-    float p = a.top_p ? a.top_p[b] : 0.0f;
-    const float min_p = a.min_p ? fminf(a.min_p[b], 1.0f) : 0.0f;
-    if (!(k > 0 && (uint32_t)k < a.V)) k = 0;
-    if (!(p > 0.0f && p < 1.0f)) p = 0.0f;
-    if (k > 0 || p > 0.0f || min_p > 0.0f) {
-      draw_filtered<DT, W>(a, b, r, k, p, (double)min_p, lds, s);
+    if (!w.is_plain()) {
+      draw_filtered<DT, W, kJoin>(a, b, r, w.f, lds, s);
       return;
     }
   }
-  draw_plain<DT, W>(a, b, r, lds, s);
+  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
+  double* sums = (double*)(lds + (DT == ESPO_BF16 ? kTableBytes : 0));
+  float* refs = (float*)(sums + chunks);
+  float top;
+  if constexpr (kJoin) {
+    const double* from = (const double*)a.split.of(b);
+    const float* from_refs = (const float*)(from + chunks);
+#pragma unroll 1
+    for (uint32_t c = threadIdx.x; c < chunks; c += W * kWave) sums[c] = from[c], refs[c] = from_refs[c];
+    top = block_max<W>(threadIdx.x < a.split.parts ? a.split.records(b)[threadIdx.x].m : kMaskedRow, s);
+  } else {
+    top = sum_plain<DT, W>(r, 0, chunks, lds, sums, refs, s);
+  }
+  draw_plain<DT, W>(a, b, r, top, sums, refs, s);
+}
+
+// One of the workgroups that a row is split over where there are few rows: its share of the row's chunks.
+constexpr int kPartWaves = 16;
+template <int DT, bool kFilters>
+__global__ __launch_bounds__(kPartWaves* kWave) void espo_sample_part_kernel(SampleArgs a) {
+  constexpr int W = kPartWaves, kThreads = W * kWave;
+  __shared__ SampleShared<W> s;
+  extern __shared__ __align__(16) unsigned char lds[];
+  const uint32_t parts = a.split.parts, part = blockIdx.x % parts;
+  const int64_t b = blockIdx.x / parts;
+  if (a.alive && !a.alive[b]) return;
+  const RowPlan w = row_plan<DT>(a, b);
+  if (w.is_greedy()) return;                // its draw reads the row itself
+  Row r = row_of<DT>(a, b, w.T);
+  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk, each = (chunks + parts - 1) / parts, c0 = part * each, c1 = min(c0 + each, chunks);
+  PartRecord* record = a.split.records(b) + part;
+  if (c0 >= c1) {                           // nothing left of the row: no logits, and empty bins
+    if (threadIdx.x == 0) *record = PartRecord{0.0, kMaskedRow, 0.0f};
+    if constexpr (kFilters) {
+      if (!w.is_plain())
+        for (uint32_t i = threadIdx.x; i < a.split.bins / 16; i += kThreads) ((u32x4*)a.split.part_bins(b, part))[i] = u32x4{0, 0, 0, 0};
+    }
+    return;
+  }
+  if constexpr (kFilters) {
+    if (!w.is_plain()) {
+      const uint32_t per = kChunk * (kWave / kBlockVecs), t1 = min(c1 * kChunk, r.ntiles);
+      float* blocks = (float*)(lds + a.lds_blocks);  // of the whole row, as far as it is this workgroup's
+      double next_to_0 = 0.0, all;
+      const float top = block_max<W>(fill_bins<DT, W>(r, c0 * kChunk, t1, w.f, lds, blocks, next_to_0), s);
+      block_before<W>(next_to_0, s.wave_f64[0], all);
+      if (threadIdx.x == 0) *record = PartRecord{all, top, 0.0f};
+      float* to = (float*)a.split.of(b);
+      for (uint32_t j = c0 * per + threadIdx.x; j < t1 * (kWave / kBlockVecs); j += kThreads) to[j] = blocks[j];
+      const uint32_t first = w.f.counts ? 0 : kCountBytes / 16, last = (uint32_t)(w.f.masses ? a.split.bins : w.f.counts ? kCountBytes : 0) / 16;
+      for (uint32_t i = first + threadIdx.x; i < last; i += kThreads) ((u32x4*)a.split.part_bins(b, part))[i] = ((const u32x4*)lds)[i];
+      return;
+    }
+  }
+  double* sums = (double*)a.split.of(b);
+  const float top = sum_plain<DT, W>(r, c0, c1, lds, sums, (float*)(sums + chunks), s);
+  if (threadIdx.x == 0) *record = PartRecord{0.0, top, 0.0f};
 }
 
 // Dynamic LDS of a draw without filters: the weights of all bins, the chunks' sums and references.
@@ -926,7 +1118,7 @@ size_t plain_lds(int64_t V) {
 template <int DT>
 size_t filter_lds(int64_t V, uint32_t& blocks, uint32_t& members) {
   const size_t E = vec_elems<DT>(), ntiles = (V + kWave * E - 1) / (kWave * E), nblocks = ntiles * (kWave / kBlockVecs);
-  const size_t bins = (size_t)(kBins + 3) / 4 * 16 + (DT == ESPO_BF16 ? 0 : (size_t)kBins * 8), visited = (nblocks + 3) / 4 * 16 + nblocks * 8;
+  const size_t bins = kCountBytes + (DT == ESPO_BF16 ? 0 : (size_t)kBins * 8), visited = (nblocks + 3) / 4 * 16 + nblocks * 8;
   size_t first = (size_t)kLevelBins * 12;
   for (size_t n : {bins, visited, plain_lds<DT>(V)}) first = n > first ? n : first;
   first = (first + 15) / 16 * 16;
@@ -935,27 +1127,67 @@ size_t filter_lds(int64_t V, uint32_t& blocks, uint32_t& members) {
   return members + (size_t)kMostMembers * 4;
 }
 
-template <int DT, int W>
-void launch(SampleArgs& a, int64_t B, hipStream_t stream) {
-  if (a.top_k || a.top_p || a.min_p) {
-    const size_t lds = filter_lds<DT>(a.V, a.lds_blocks, a.lds_members);
-    hipLaunchKernelGGL((espo_sample_kernel<DT, W, true>), dim3((unsigned)B), dim3(W * kWave), lds, stream, a);
+constexpr int64_t kComputeUnits = 256, kMostParts = 8, kPartTiles = 64;
+
+// Workgroups that a row is split over: as many as the idle compute units allow, of at least 64 tiles each (four per wave).
+template <int DT>
+uint32_t parts_of(int64_t B, int64_t V) {
+  const int64_t tiles = V / (kWave * vec_elems<DT>());
+  int64_t n = kComputeUnits / B;
+  if (n > tiles / kPartTiles) n = tiles / kPartTiles;
+  if (n > kMostParts) n = kMostParts;
+  return n < 2 || V > (1 << 19) ? 1u : (uint32_t)n;
+}
+
+template <int DT>
+SplitLayout split_layout(int64_t B, int64_t V) {
+  const size_t tile = kWave * vec_elems<DT>(), ntiles = (V + tile - 1) / tile, chunks = (ntiles + kChunk - 1) / kChunk;
+  size_t front = ntiles * (kWave / kBlockVecs) * 4;
+  if (front < chunks * 12) front = chunks * 12;
+  front = (front + 15) / 16 * 16;
+  SplitLayout l{nullptr, 0, kCountBytes + (DT == ESPO_BF16 ? 0 : (size_t)(kBins + 1) / 2 * 16), parts_of<DT>(B, V), (uint32_t)front};
+  l.row = (front + l.parts * (sizeof(PartRecord) + l.bins) + 255) / 256 * 256;
+  return l;
+}
+
+template <int DT, bool kFilters>
+void launch(SampleArgs& a, int64_t B, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const size_t lds = kFilters ? filter_lds<DT>(a.V, a.lds_blocks, a.lds_members) : plain_lds<DT>(a.V);
+  a.split = split_layout<DT>(B, a.V);
+  if (a.split.parts > 1 && workspace && workspace_bytes >= (size_t)B * a.split.row && (uintptr_t)workspace % 16 == 0) {
+    a.split.base = (char*)workspace;
+    hipLaunchKernelGGL((espo_sample_part_kernel<DT, kFilters>), dim3((unsigned)(B * a.split.parts)), dim3(kPartWaves * kWave), lds, stream, a);
+    hipLaunchKernelGGL((espo_sample_kernel<DT, 16, kFilters, true>), dim3((unsigned)B), dim3(16 * kWave), lds, stream, a);
+  } else if (B <= kComputeUnits) {
+    hipLaunchKernelGGL((espo_sample_kernel<DT, 16, kFilters, false>), dim3((unsigned)B), dim3(16 * kWave), lds, stream, a);
   } else {
-    hipLaunchKernelGGL((espo_sample_kernel<DT, W, false>), dim3((unsigned)B), dim3(W * kWave), plain_lds<DT>(a.V), stream, a);
+    hipLaunchKernelGGL((espo_sample_kernel<DT, 8, kFilters, false>), dim3((unsigned)B), dim3(8 * kWave), lds, stream, a);
   }
+}
+
+template <int DT>
+void launch(SampleArgs& a, int64_t B, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (a.top_k || a.top_p || a.min_p)
+    launch<DT, true>(a, B, workspace, workspace_bytes, stream);
+  else
+    launch<DT, false>(a, B, workspace, workspace_bytes, stream);
 }
 
 }  // namespace
 
+size_t sample_workspace(int dt, int64_t B, int64_t V) {
+  const SplitLayout l = dt == ESPO_BF16 ? split_layout<ESPO_BF16>(B, V) : split_layout<ESPO_F32>(B, V);
+  return l.parts > 1 ? (size_t)B * l.row : 0;
+}
+
 int launch_sample(const void* logits, int dt, int64_t B, int64_t V, int64_t row_stride, const float* temperature, const int32_t* top_k,
                   const float* top_p, const float* min_p, const float* u, const uint8_t* alive, int32_t* tokens, float* logprob,
-                  hipStream_t stream) {
-  SampleArgs a{(const char*)logits, row_stride * (dt == ESPO_BF16 ? 2 : 4), (uint32_t)V, temperature, top_k, top_p, min_p, u, alive, tokens, logprob, 0, 0};
-  const bool many = B > 256;
+                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  SampleArgs a{(const char*)logits, row_stride * (dt == ESPO_BF16 ? 2 : 4), (uint32_t)V, temperature, top_k, top_p, min_p, u, alive, tokens, logprob, 0, 0, {}};
   if (dt == ESPO_BF16)
-    many ? launch<ESPO_BF16, 8>(a, B, stream) : launch<ESPO_BF16, 16>(a, B, stream);
+    launch<ESPO_BF16>(a, B, workspace, workspace_bytes, stream);
   else
-    many ? launch<ESPO_F32, 8>(a, B, stream) : launch<ESPO_F32, 16>(a, B, stream);
+    launch<ESPO_F32>(a, B, workspace, workspace_bytes, stream);
   return hipGetLastError() == hipSuccess ? ESPO_OK : ESPO_EHIP;
 }
 
