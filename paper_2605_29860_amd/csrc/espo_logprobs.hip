@@ -21,7 +21,10 @@ constexpr int kRowWaves = 8, kRowThreads = kRowWaves * kWave;
 constexpr int kGradThreads = 256, kGradLoads = 4;
 constexpr int kGradSpan = kGradThreads * kGradLoads;  // vectors of a workgroup
 constexpr int kComputeUnits = 256;
-constexpr int64_t kHeldRows = 192;               // fewer rows leave compute units idle where one workgroup holds a row
+// Rows are held by a workgroup each from this many waves on (the chip has 4096 at a time); fewer leave compute units idle, and two passes of
+// smaller workgroups are faster.  us, held / two passes: V = 152064 bf16 (16 waves) N = 64 30.9 / 25.8, 96 31.4 / 30.4, 128 32.1 / 34.9,
+// 256 37.6 / 46.9; V = 32768 f32 (8 waves) N = 160 17.7 / 18.0, 256 19.0 / 24.4; V = 32000 bf16 (4 waves) N = 256 17.7 / 16.3, 512 21.5 / 24.7.
+constexpr int64_t kHeldWaves = 1600;
 constexpr int kSumThreads = 1024, kSumWaves = kSumThreads / kWave;
 
 struct RowArgs {
@@ -466,8 +469,8 @@ void policy_held(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const
 // Log-probabilities, entropy and, if it is wanted, the gradient of the objective.
 template <int DT>
 void policy(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, hipStream_t stream) {
-  const int waves = d.dlogits && a.N >= kHeldRows ? held_waves<DT>(a.V) : 0;
-  switch (waves) {
+  const int waves = d.dlogits ? held_waves<DT>(a.V) : 0;
+  switch (a.N * waves >= kHeldWaves ? waves : 0) {
     case 4: return policy_held<DT, 4>(a, o, d, q, stream);
     case 8: return policy_held<DT, 8>(a, o, d, q, stream);
     case 16: return policy_held<DT, 16>(a, o, d, q, stream);

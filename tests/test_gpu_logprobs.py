@@ -162,7 +162,8 @@ def loss_inputs(f, N, g, spread=0.15):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("N,V,T,coef,weighted", [(1, 5, 1.0, 0.0, False), (7, 4096, 1.0, 0.01, True), (40, 50003, 0.6, 0.0, True), (300, 1003, 1.0, 0.02, False),
                                                  (257, 33000, 1.0, 0.5, False), (260, 70001, 1.0, 0.0, True), (256, 152064, 0.8, 0.01, False),
-                                                 (1500, 9, 1.0, 0.1, True), (530, 82001, 0.9, 0.0, False), (600, 8192, 1.0, 0.01, False), (192, 38912, 1.0, 0.0, True), (260, 19457, 1.0, 0.01, False),
+                                                 (1500, 9, 1.0, 0.1, True), (530, 82001, 0.9, 0.0, False), (600, 8192, 1.0, 0.01, False), (192, 38912, 1.0, 0.0, True), (260, 19457, 1.0, 0.01, False), (450, 38912, 1.0, 0.0, True), (110, 140001, 1.0, 0.01, False),
+                                                 (210, 77825, 1.0, 0.0, False), (700, 19457, 1.0, 0.01, True),
                                                  (1100, 5121, 1.0, 0.01, False)])
 def test_policy_loss(N, V, T, coef, weighted, dtype):
     print(f"[case] policy loss N={N} V={V} T={T} coef={coef} {dtype}", flush=True)
