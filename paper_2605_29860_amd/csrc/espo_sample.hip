@@ -61,6 +61,11 @@ __device__ __forceinline__ uint32_t bins_of_pair(uint32_t w) {
   const i16x2 b = (__builtin_bit_cast(i16x2, j) ^ s) - s;
   return __builtin_bit_cast(uint32_t, __builtin_bit_cast(u16x2, b) * (unsigned short)kEntry + (u16x2)(unsigned short)(kBinZero * kEntry));
 }
+// The smaller one of two numbers of 16 bits, in both halves.
+__device__ __forceinline__ uint32_t min_of_pairs(uint32_t a, uint32_t b) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
 // The number of a bin: the one nearest to 0 that falls into it.
 __device__ __forceinline__ float bin_number(int bin) {
   const int j = bin - kBinZero;
@@ -471,9 +476,9 @@ __device__ __forceinline__ void stream_chunks(const RowView& r, uint32_t c0, uin
 
 // The kept sum of every chunk of bf16 logits, with weights from a table of all bins: 2^((x - base) c), 0 of what is not kept.  A look-up takes
 // less than half the time of a power of 2 in double (B = 512, V = 152064: 62 -> 46 us).  Logits next to 0, of which one bin
-// holds many, are weighed one by one; the two bins at the ends, of all beyond 128, count as nothing, and the caller sees to it that they may.
-// Weights are relative to r.m, the row's largest logit, or if that is not known (`find`) to the largest one of the waves' first tiles, which
-// r.m then becomes: any logit near the top does.  Returns the thread's largest logit, +inf if the table's numbers would be too large.
+// holds many, are weighed one by one; those of -128 and less count as nothing, and the caller sees to it that they may.  Weights are relative to
+// r.m, the row's largest logit, or if that is not known (`find`) to the largest one of the waves' first tiles, which r.m then becomes: any
+// logit near the top does.  Returns the largest of what the thread's sums are: 0 nothing, 1 numbers, 2 no use (a logit of 128 or more).
 template <int W>
 __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, const Kept& keep, bool find, unsigned char* lds, double* sums, SampleShared<W>& s) {
   constexpr uint32_t E = vec_elems<ESPO_BF16>();
@@ -482,7 +487,7 @@ __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, 
     const double w = r.weight(x);
     return x >= keep.cut && w >= keep.min_p ? w : 0.0;
   };
-  float m = kMaskedRow;
+  float is = 0.0f;
   double sum = 0.0;
   stream_chunks<W>(
       r, c0, c1,
@@ -492,33 +497,34 @@ __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, 
           tile_logits<ESPO_BF16>(r, t, raw, y);
           const float top = block_max<W>(max_of<E>(y), s);
           r.m = top > kMaskedRow ? (double)top : 0.0;
-          if (!(((double)kBinsBelow - r.m) * r.c < 1000.0)) {
-            m = __builtin_huge_valf();
+          if (!(((double)kBinsBelow - r.m) * r.c < 1000.0)) {  // weights would not be numbers
+            is = 2.0f;
             return false;
           }
         }
 #pragma unroll 1
-        for (int i = threadIdx.x; i < kBins; i += W * kWave) table[i] = i > 1 && i < kBins - 2 && i != kBinZero ? weight(bin_number(i)) : 0.0;
+        for (int i = threadIdx.x; i < kBins; i += W * kWave)
+          table[i] = i > 1 && i < kBins - 2 && i != kBinZero ? weight(bin_number(i)) : i == kBins - 2 ? __builtin_huge_val() : 0.0;
         __syncthreads();
         return true;
       },
       [&](uint32_t t, u32x4 raw) {
-        float y[E];
-        tile_logits<ESPO_BF16>(r, t, raw, y);
-        if (t + 1 >= r.ntiles) raw = vec_pack<ESPO_BF16>(y);
-        m = fmaxf(m, max_of<E>(y));
-        float least = fabsf(y[0]);
-#pragma unroll
-        for (uint32_t j = 1; j < E; ++j) least = fminf(least, fabsf(y[j]));
+        if (t + 1 >= r.ntiles) {
+          float y[E];
+          tile_logits<ESPO_BF16>(r, t, raw, y);
+          raw = vec_pack<ESPO_BF16>(y);
+        }
+        uint32_t least = 0x7fff7fffu;       // of both halves, without the sign
         double w[E];
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
           const uint32_t at = bins_of_pair<8>(raw[j]);
+          least = min_of_pairs(least, raw[j] & 0x7fff7fffu);
           w[2 * j] = *(const double*)(lds + (at & 0xffffu));
           w[2 * j + 1] = *(const double*)(lds + (at >> 16));
         }
         sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-        if (__builtin_amdgcn_ballot_w64(least < 0x1p-10f) != 0) {
+        if (__builtin_amdgcn_ballot_w64((least & 0xffffu) <= kMagBelow || (least >> 16) <= kMagBelow) != 0) {
 #pragma unroll 1
           for (uint32_t j = 0; j < E; ++j) {
             const float x = logit_in<ESPO_BF16>(raw, j);
@@ -529,9 +535,10 @@ __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, 
       [&](uint32_t c) {
         sum = wave_sum_f64(sum);
         if (threadIdx.x % kWave == 0) sums[c] = sum;
+        is = fmaxf(is, sum > 1e300 ? 2.0f : sum > kNoWeight ? 1.0f : 0.0f);
         sum = 0.0;
       });
-  return m;
+  return is;
 }
 
 // The same with a power of 2 for every logit.  Without a filter the largest logit is not known before: the sums are then
@@ -576,23 +583,24 @@ __device__ __forceinline__ float sum_by_powers(const Row& r, uint32_t c0, uint32
 
 constexpr size_t kTableBytes = (size_t)(kBins + 1) / 2 * 16;
 
-// No filter: the sums of chunks c0 .. c1 - 1 (sums[0] is chunk 0's), and what each is relative to.  Returns the largest logit.
+// No filter: the sums of chunks c0 .. c1 - 1 (sums[0] is chunk 0's), and what each is relative to.  Returns the largest of these references, which is
+// the largest logit or near it; kMaskedRow if there is no logit.
 template <int DT, int W>
 __device__ __forceinline__ float sum_plain(Row& r, uint32_t c0, uint32_t c1, unsigned char* lds, double* sums, float* refs, SampleShared<W>& s) {
   const Kept all{-3.402823466e38f, 0.0};
   if constexpr (DT == ESPO_BF16) {
-    const float top = block_max<W>(sum_by_table<W>(r, c0, c1, all, true, lds, sums, s), s);
+    const float is = block_max<W>(sum_by_table<W>(r, c0, c1, all, true, lds, sums, s), s);
     __syncthreads();
-    if (!(top > kMaskedRow) || (top < kBinsBelow && ((double)top + kBinsBelow) * r.inv_t > 50.0)) {
+    if (is == 1.0f && (r.m + (double)kBinsBelow) * r.inv_t > 50.0) {
 #pragma unroll 1
-      for (uint32_t c = c0 + threadIdx.x; c < c1; c += W * kWave) refs[c] = top > kMaskedRow ? (float)r.m : kMaskedRow;
-      return top;
+      for (uint32_t c = c0 + threadIdx.x; c < c1; c += W * kWave) refs[c] = (float)r.m;
+      return (float)r.m;
     }
   }
   return block_max<W>(sum_by_powers<DT, W, false>(r, c0, c1, all, sums, refs), s);
 }
 
-// Its draw, once the largest logit is known and the sums are in LDS.
+// Its draw, once the sums are in LDS.
 template <int DT, int W>
 __device__ __forceinline__ void draw_plain(const SampleArgs& a, int64_t b, Row& r, float top, double* sums, const float* refs, SampleShared<W>& s) {
   const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk;
@@ -1077,16 +1085,8 @@ __global__ __launch_bounds__(kPartWaves* kWave) void espo_sample_part_kernel(Sam
   const RowPlan w = row_plan<DT>(a, b);
   if (w.is_greedy()) return;                // its draw reads the row itself
   Row r = row_of<DT>(a, b, w.T);
-  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk, each = (chunks + parts - 1) / parts, c0 = part * each, c1 = min(c0 + each, chunks);
+  const uint32_t chunks = (r.ntiles + kChunk - 1) / kChunk, each = (chunks + parts - 1) / parts, c0 = part * each, c1 = min(c0 + each, chunks);  // at least 8 chunks a part, 8 parts at most: none is empty
   PartRecord* record = a.split.records(b) + part;
-  if (c0 >= c1) {                           // nothing left of the row: no logits, and empty bins
-    if (threadIdx.x == 0) *record = PartRecord{0.0, kMaskedRow, 0.0f};
-    if constexpr (kFilters) {
-      if (!w.is_plain())
-        for (uint32_t i = threadIdx.x; i < a.split.bins / 16; i += kThreads) ((u32x4*)a.split.part_bins(b, part))[i] = u32x4{0, 0, 0, 0};
-    }
-    return;
-  }
   if constexpr (kFilters) {
     if (!w.is_plain()) {
       const uint32_t per = kChunk * (kWave / kBlockVecs), t1 = min(c1 * kChunk, r.ntiles);
@@ -1127,25 +1127,31 @@ size_t filter_lds(int64_t V, uint32_t& blocks, uint32_t& members) {
   return members + (size_t)kMostMembers * 4;
 }
 
-constexpr int64_t kComputeUnits = 256, kMostParts = 8, kPartTiles = 64;
-
-// Workgroups that a row is split over: as many as the idle compute units allow, of at least 64 tiles each (four per wave).
+// Workgroups that a row is split over: as many as the idle compute units allow, of enough tiles each.  A draw without filters gains from
+// 32 tiles each on (two per wave), bf16 logits in rows of 256 tiles; a filtered one, whose parts hand their bins on, in
+// rows of 256 tiles and from three parts of 64 tiles on.  us, whole rows / split (T = 1): V = 152064 bf16, plain B = 1 21.5 / 14.7, 64 23.8 / 18.5,
+// 128 24.5 / 22.4; nucleus of 0.7 B = 1 25.6 / 21.7, 64 29.5 / 28.1, 128 30.3 / 31.5 in two parts; V = 152064 f32, B = 32: plain 32.8 / 14.2,
+// nucleus 80 / 51; V = 50003 bf16, B = 32, in three parts: plain 14.7 / 16.1, nucleus 18.5 / 21.0; V = 32768 f32, B = 4: plain 11.5 / 10.3, top-k 50
+// in two parts 16.1 / 18.8.
+constexpr int64_t kComputeUnits = 256, kMostParts = 8;
 template <int DT>
-uint32_t parts_of(int64_t B, int64_t V) {
+uint32_t parts_of(int64_t B, int64_t V, bool filters) {
   const int64_t tiles = V / (kWave * vec_elems<DT>());
+  if (V > (1 << 19) || ((filters || DT == ESPO_BF16) && tiles < 256)) return 1;
   int64_t n = kComputeUnits / B;
-  if (n > tiles / kPartTiles) n = tiles / kPartTiles;
+  if (n > tiles / (filters ? 64 : 32)) n = tiles / (filters ? 64 : 32);
   if (n > kMostParts) n = kMostParts;
-  return n < 2 || V > (1 << 19) ? 1u : (uint32_t)n;
+  return n < (filters ? 3 : 2) ? 1u : (uint32_t)n;
 }
 
 template <int DT>
-SplitLayout split_layout(int64_t B, int64_t V) {
+SplitLayout split_layout(int64_t B, int64_t V, bool filters) {
   const size_t tile = kWave * vec_elems<DT>(), ntiles = (V + tile - 1) / tile, chunks = (ntiles + kChunk - 1) / kChunk;
   size_t front = ntiles * (kWave / kBlockVecs) * 4;
   if (front < chunks * 12) front = chunks * 12;
   front = (front + 15) / 16 * 16;
-  SplitLayout l{nullptr, 0, kCountBytes + (DT == ESPO_BF16 ? 0 : (size_t)(kBins + 1) / 2 * 16), parts_of<DT>(B, V), (uint32_t)front};
+  const size_t bins = filters ? kCountBytes + (DT == ESPO_BF16 ? 0 : (size_t)(kBins + 1) / 2 * 16) : 0;
+  SplitLayout l{nullptr, 0, bins, parts_of<DT>(B, V, filters), (uint32_t)front};
   l.row = (front + l.parts * (sizeof(PartRecord) + l.bins) + 255) / 256 * 256;
   return l;
 }
@@ -1153,7 +1159,7 @@ SplitLayout split_layout(int64_t B, int64_t V) {
 template <int DT, bool kFilters>
 void launch(SampleArgs& a, int64_t B, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   const size_t lds = kFilters ? filter_lds<DT>(a.V, a.lds_blocks, a.lds_members) : plain_lds<DT>(a.V);
-  a.split = split_layout<DT>(B, a.V);
+  a.split = split_layout<DT>(B, a.V, kFilters);
   if (a.split.parts > 1 && workspace && workspace_bytes >= (size_t)B * a.split.row && (uintptr_t)workspace % 16 == 0) {
     a.split.base = (char*)workspace;
     hipLaunchKernelGGL((espo_sample_part_kernel<DT, kFilters>), dim3((unsigned)(B * a.split.parts)), dim3(kPartWaves * kWave), lds, stream, a);
@@ -1176,8 +1182,12 @@ void launch(SampleArgs& a, int64_t B, void* workspace, size_t workspace_bytes, h
 }  // namespace
 
 size_t sample_workspace(int dt, int64_t B, int64_t V) {
-  const SplitLayout l = dt == ESPO_BF16 ? split_layout<ESPO_BF16>(B, V) : split_layout<ESPO_F32>(B, V);
-  return l.parts > 1 ? (size_t)B * l.row : 0;
+  size_t most = 0;
+  for (bool filters : {false, true}) {
+    const SplitLayout l = dt == ESPO_BF16 ? split_layout<ESPO_BF16>(B, V, filters) : split_layout<ESPO_F32>(B, V, filters);
+    if (l.parts > 1 && (size_t)B * l.row > most) most = (size_t)B * l.row;
+  }
+  return most;
 }
 
 int launch_sample(const void* logits, int dt, int64_t B, int64_t V, int64_t row_stride, const float* temperature, const int32_t* top_k,
