@@ -545,7 +545,7 @@ size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
  *   N, V        N >= 0 (0 is a no-op), V >= 1; N < 2^31, V <= 2^30, and for the gradient N * ceil(V / 8192) < 2^31
  *               (bf16; V / 4096 for fp32) (ESPO_ERANGE).
  *   row_stride  elements between rows, >= V.
- *   temperature between 1e-30 and 1e26.
+ *   temperature between 1e-6 and 1e26.
  *   tokens      device, [N] int32.
  *   logprob     device, [N] fp32 out.
  *   entropy     device, [N] fp32 out, may be NULL (then nothing is spent on it).  For espo_logprobs_backward an input,

@@ -45,10 +45,11 @@ __device__ __forceinline__ bool used_row(int32_t token, uint32_t V) { return (ui
 // What a row's sums come to.  A row without any logit has the statistics of an empty sum, and its token is masked.
 __device__ __forceinline__ void row_results(const RowArgs& a, float x_token, const SoftmaxSums& p, float& logprob, float& entropy, float2& stats) {
   const bool any = p.m > kMaskedRow;
-  const float ln_s = any ? logf(p.s) : 0.0f;
+  const SoftmaxSums q = exact_sums(p, a.k2);
+  const float ln_s = any ? logf(q.s) : 0.0f;
   logprob = x_token > kMaskedRow ? -(p.m - x_token) * a.inv_t - ln_s : kNegInf;
-  entropy = any ? ln_s - p.a * __builtin_amdgcn_rcpf(p.s) * kLn2 : 0.0f;
-  stats = any ? float2{p.m, p.s} : float2{0.0f, 1.0f};
+  entropy = any ? ln_s - q.a * __builtin_amdgcn_rcpf(q.s) * kLn2 : 0.0f;
+  stats = any ? float2{p.m, q.s} : float2{0.0f, 1.0f};
 }
 
 __device__ __forceinline__ void store_row(const RowOutputs& o, int64_t row, float logprob, float entropy, float2 stats) {
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(kRowThreads) void espo_logprobs_kernel(RowArgs a, R
   }
   const char* x = a.logits + row * a.row_bytes;
   const RowView r = row_view<DT>(x, a.V);
-  SoftmaxSums p{kMaskedRow, 0.0f, 0.0f};
+  SoftmaxSums p = kNoSums;
   stream_tiles(r, threadIdx.x >> 6, r.ntiles, kRowWaves, [&](uint32_t t, const u32x4* raw) {
     float y[kAhead][E], m = p.m;
 #pragma unroll
@@ -128,15 +129,17 @@ __device__ __forceinline__ Surrogate surrogate(const PolicyArgs& q, const TokenI
   return c;
 }
 
-// A row's gradient: dx_v = 2^t (p0 + p1 t) with t = (x_v - m) k2, and `at` more at the token.
+// A row's gradient: dx_v = 2^t (p0 + p1 t) with t = x_v k2 + nb, and `at` more at the token.
 struct RowGrad {
-  float m, p0, p1, at;
+  float nb, p0, p1, at;
 };
 
 // m, s: the row's largest logit and sum; `entropy` only counts where h is not 0.
 __device__ __forceinline__ RowGrad row_grad(const RowArgs& a, float m, float s, float entropy, float g, float h) {
-  const float per = a.inv_t * __builtin_amdgcn_rcpf(s);
-  return RowGrad{m, -(h != 0.0f ? g + h * (entropy - logf(s)) : g) * per, -h * kLn2 * per, g * a.inv_t};
+#pragma clang fp contract(off)  // nb is a rounded product
+  const float nb = -m * a.k2, d = exponent_short(m, nb, a.k2);  // t is short by the rounding of nb, and 2^t by a factor
+  const float per = a.inv_t * __builtin_amdgcn_rcpf(s) * __builtin_amdgcn_exp2f(d), p1 = -h * kLn2 * per;
+  return RowGrad{nb, p1 * d - (h != 0.0f ? g + h * (entropy - logf(s)) : g) * per, p1, g * a.inv_t};
 }
 
 template <int DT, bool kSlope>
@@ -148,7 +151,7 @@ __device__ __forceinline__ u32x4 grad_vec(const RowArgs& a, const RowGrad& c, u3
 #pragma unroll
   for (int k = 0; k < E; ++k) {
     const float x = y[k];
-    float t = (x - c.m) * a.k2;
+    float t = __builtin_fmaf(x, a.k2, c.nb);
     if constexpr (kSlope) t = fmaxf(t, kLeastExponent);
     const float e = __builtin_amdgcn_exp2f(t);
     y[k] = e * (kSlope ? __builtin_fmaf(c.p1, t, c.p0) : c.p0);
@@ -309,7 +312,7 @@ __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))
     const int32_t token = __builtin_amdgcn_readfirstlane(rows.token[i]);
     const int token_round = (int)((uint32_t)token / E / kThreads);
     const bool holds_token = threadIdx.x == (uint32_t)token / E % kThreads;
-    SoftmaxSums p{kMaskedRow, 0.0f, 0.0f};
+    SoftmaxSums p = kNoSums;
     u32x4 tail = vec_masked<DT>();
 #pragma unroll
     for (int r = 0; r < kHeld; ++r) {

@@ -135,16 +135,19 @@ __device__ __forceinline__ void stream_tiles(const RowView& r, uint32_t first, u
     return __builtin_nontemporal_load((const u32x4*)(r.x + (size_t)min(t * kWave + lane, r.nvec - 1) * 16));
   };
   if (first >= end) return;
-  u32x4 cur[kAhead], nxt[kAhead];
+  u32x4 a[kAhead], b[kAhead];
+  const auto load_all = [&](u32x4* v, uint32_t t) {
 #pragma unroll
-  for (int j = 0; j < kAhead; ++j) cur[j] = load(first + j * step);
-#pragma unroll 1
-  for (uint32_t t = first; t < end; t += kAhead * step) {
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) nxt[j] = load(min(t + (kAhead + j) * step, end - 1));
-    use(t, cur);
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) cur[j] = nxt[j];
+    for (int j = 0; j < kAhead; ++j) v[j] = load(min(t + j * step, end - 1));
+  };
+  load_all(a, first);
+  for (uint32_t t = first;;) {
+    load_all(b, t + kAhead * step);
+    use(t, a);
+    if ((t += kAhead * step) >= end) return;
+    load_all(a, t + kAhead * step);
+    use(t, b);
+    if ((t += kAhead * step) >= end) return;
   }
 }
 
@@ -169,19 +172,24 @@ __device__ __forceinline__ float logit_at(const char* row, uint32_t v) {
     return ((const float*)row)[v];
 }
 
-// Softmax sums relative to the largest logit seen: s = sum 2^t, a = sum t 2^t with t = (x - m) k2, k2 = log2(e) / temperature.
-// The difference x - m is formed first: as x k2 - m k2 the rounding of m k2 would scale a lane's sums by a factor of its own.
-// m starts at kMaskedRow, and sums of a lane that has seen nothing above it are dropped when lanes are merged.
+// Softmax sums of the logits seen so far: s = sum 2^t, a = sum t 2^t with t = x k2 + nb, k2 = log2(e) / temperature and nb = -m k2
+// rounded, m the largest logit.  One fused operation forms t, with an error of 2^-24 |t| however large m k2 is; that nb is rounded
+// scales both sums by one factor, which exact_sums takes out.  m starts at kMaskedRow, and sums over nothing but masked
+// logits are dropped.
 struct SoftmaxSums {
-  float m, s, a;
+  float m, nb, s, a;
 };
+constexpr SoftmaxSums kNoSums = SoftmaxSums{kMaskedRow, 0.0f, 0.0f, 0.0f};
 
 template <bool kEntropy>
 __device__ __forceinline__ void rescale(SoftmaxSums& p, float m, float k2) {
-  const float d = fmaxf((p.m - m) * k2, kLeastExponent), f = __builtin_amdgcn_exp2f(d);
-  if constexpr (kEntropy) p.a = f * (p.a + d * p.s);
-  p.s *= f;
+#pragma clang fp contract(off)  // the difference of two references is that of their rounded values
+  const bool any = p.m > kMaskedRow;
+  const float nb = -m * k2, d = fmaxf(nb - p.nb, kLeastExponent), f = any ? __builtin_amdgcn_exp2f(d) : 0.0f, s = any ? p.s : 0.0f;
+  if constexpr (kEntropy) p.a = f * ((any ? p.a : 0.0f) + d * s);
+  p.s = s * f;
   p.m = m;
+  p.nb = nb;
 }
 
 // The same where one of the lanes needs it: after a row's first vectors hardly any does.
@@ -192,19 +200,17 @@ __device__ __forceinline__ void follow(SoftmaxSums& p, float m, float k2) {
 
 template <bool kEntropy>
 __device__ __forceinline__ void add_logit(SoftmaxSums& p, float x, float k2) {
-  float t = (x - p.m) * k2;
+  float t = __builtin_fmaf(x, k2, p.nb);
   if constexpr (kEntropy) t = fmaxf(t, kLeastExponent);
   const float e = __builtin_amdgcn_exp2f(t);
   p.s += e;
-  if constexpr (kEntropy) p.a += e * t;
+  if constexpr (kEntropy) p.a = __builtin_fmaf(e, t, p.a);
 }
 
 // Merged over a wave, wave-uniform, in a fixed order.
 template <bool kEntropy>
 __device__ __forceinline__ SoftmaxSums wave_merge(SoftmaxSums p, float k2) {
-  const float m = wave_max(p.m);
-  if (!(p.m > kMaskedRow)) p.s = p.a = 0.0f;
-  rescale<kEntropy>(p, m, k2);
+  rescale<kEntropy>(p, wave_max(p.m), k2);
   p.s = wave_sum(p.s);
   if constexpr (kEntropy) p.a = wave_sum(p.a);
   return p;
@@ -217,7 +223,18 @@ __device__ __forceinline__ SoftmaxSums block_merge(SoftmaxSums p, float k2, Soft
   const int lane = threadIdx.x & (kWave - 1);
   if (lane == 0) lds[threadIdx.x >> 6] = p;
   __syncthreads();
-  return wave_merge<kEntropy>(lane < W ? lds[lane] : SoftmaxSums{kMaskedRow, 0.0f, 0.0f}, k2);
+  return wave_merge<kEntropy>(lane < W ? lds[lane] : kNoSums, k2);
+}
+
+// By how much t falls short of (x - m) k2.
+__device__ __forceinline__ float exponent_short(float m, float nb, float k2) { return __builtin_fmaf(-m, k2, -nb); }
+
+// The sums relative to m itself.  The largest logit's own term is 1, and 0 in a, by definition: it is taken out as it was added and put
+// back as that, so that a row of one logit has the sums 1 and 0.
+__device__ __forceinline__ SoftmaxSums exact_sums(const SoftmaxSums& p, float k2) {
+  const float d = exponent_short(p.m, p.nb, k2), f = __builtin_amdgcn_exp2f(d), t = __builtin_fmaf(p.m, k2, p.nb), e = __builtin_amdgcn_exp2f(t);
+  const float s = p.s - e, a = p.a - e * t;
+  return SoftmaxSums{p.m, p.nb, __builtin_fmaf(s, f, 1.0f), f * __builtin_fmaf(d, s, a)};
 }
 
 }  // namespace espo

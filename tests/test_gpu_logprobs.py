@@ -94,10 +94,30 @@ def test_shapes(N, V, T, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("T", [1e-3, 0.1, 50.0, 1e6])
+@pytest.mark.parametrize("T", [1e-6, 1e-3, 0.1, 50.0, 1e6, 1e20])
 def test_temperatures(T, dtype):
     print(f"[case] logprobs temperature {T} {dtype}", flush=True)
     check_all(4, 3001, dtype, T, seed=5)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shift", [1000.0, -5000.0, -1e6])
+def test_shifted_and_wide_logits(shift, dtype):
+    print(f"[case] logprobs shifted {shift} {dtype}", flush=True)
+    V, T = 5003, 0.7
+    x, tokens, x64, tok, g = make(5, V, dtype, 17, unused=0.0, scale=30.0)
+    x += shift
+    x[3] = torch.linspace(-90, 90, V).to(dtype).cuda()          # every part of the row has a larger logit than the one before
+    x[4] = torch.linspace(90, -90, V).to(dtype).cuda()
+    f = R.softmax_rows(x.double().cpu(), T, tok)
+    lp, H, stats = forward(x, tokens, T)
+    check(lp, f["logprob"], R.logprob_bound(f, V), "logprob")
+    check(H, f["entropy"], R.entropy_bound(f, V), "entropy")
+    w = torch.randn(5, generator=g)
+    d, _ = pitched(x)
+    espo.espo_logprobs_backward(x, T, tokens, stats, w.cuda(), d, entropy=H, dentropy=w.cuda())
+    want = R.logits_grad(f, w.double(), w.double())
+    check(d, want, R.grad_bound(f, w.double(), w.double(), want, torch.finfo(dtype).eps / 2, V), "gradient")
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])

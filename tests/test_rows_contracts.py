@@ -38,7 +38,7 @@ def test_logprobs_refusals(lib):
         logits, dt, N, V, stride, T, tokens, lp, H, stats, None, 0, None)
     assert call(N=0) == 0 and call(N=0, logits=None, tokens=None) == 0
     assert call(dt=2) == -1 and call(N=-1) == -1 and call(V=0) == -1 and call(stride=63) == -1
-    for T in (0.0, -1.0, math.nan, math.inf, 1e-31, 1e27):
+    for T in (0.0, -1.0, math.nan, math.inf, 1e-31, 9e-7, 1e27):
         assert call(T=T) == -1, T
     assert call(logits=None) == -1 and call(tokens=None) == -1 and call(lp=None) == -1
     assert call(logits=ODD) == -2 and call(V=63, stride=63) == -2 and call(stats=ODD) == -2
