@@ -41,7 +41,8 @@ constexpr double kNoWeight = 1e-250;        // weights below this count as none
 constexpr int kMagBelow = ((127 - 10) << 7) - 1;  // the bf16 number before 2^-10
 constexpr int kMagSpan = 17 << 7;                 // numbers from 2^-10 to 128
 constexpr int kBinZero = kMagSpan + 2;            // bin of everything next to 0
-constexpr int kBins = 2 * kBinZero + 1;           // the first and the last usable one, 1 and kBins - 2, stand for all beyond 128
+constexpr int kBins = 2 * kBinZero + 1;
+constexpr int kBinLow = 1, kBinHigh = kBins - 2;  // of -128 and less (not masked), of 128 and more
 constexpr float kBinsBelow = 128.0f;
 constexpr size_t kCountBytes = (size_t)(kBins + 3) / 4 * 16;
 constexpr double kBinMass = 1099511627776.0;      // 2^40: the mass of a bin is in units of 2^-40 of its own number's weight
@@ -215,8 +216,9 @@ __device__ __forceinline__ double block_before(double v, double* lds, double& to
 }
 
 // The thread whose part [before, before + v) of a running sum holds `target`: the first with before + v beyond it (or, where `reach`,
-// at it); the last with any part if rounding leaves none.  The same in all threads.  (By ballots: LDS atomics on one word are turned into a
-// loop over the lanes, 4 us here.)
+// at it); the last with any part if rounding leaves none; kNone if there is no part at all (rows with NaN only).  The same in all
+// threads.  (By ballots: LDS atomics on one word are turned into a loop over the lanes, 4 us here.)
+constexpr uint32_t kNone = 0xffffffffu;
 template <int W>
 __device__ __forceinline__ uint32_t block_pick(double before, double v, double target, bool reach, int2* lds) {
   const double upto = before + v;
@@ -229,7 +231,7 @@ __device__ __forceinline__ uint32_t block_pick(double before, double v, double t
   const int2 w = lane < W ? lds[lane] : int2{-1, -1};
   const uint64_t hits = __builtin_amdgcn_ballot_w64(w.x >= 0), somes = __builtin_amdgcn_ballot_w64(w.y >= 0);
   if (hits) return (uint32_t)__builtin_amdgcn_readlane(w.x, (int)__builtin_ctzll(hits));
-  return somes ? (uint32_t)__builtin_amdgcn_readlane(w.y, 63 - (int)__builtin_clzll(somes)) : 0u;
+  return somes ? (uint32_t)__builtin_amdgcn_readlane(w.y, 63 - (int)__builtin_clzll(somes)) : kNone;
 }
 
 // Calls use(t, raw) for tiles first, first + step, ... below end, one after the other, with the next three on their way: a loop of little
@@ -378,7 +380,12 @@ __device__ __forceinline__ void draw(const SampleArgs& a, int64_t b, const Row& 
   for (uint32_t q = q0; q < q1; ++q) mine += sums[q];
   double before = block_before<W>(mine, s.wave_f64[1], total);
   const double target = (double)a.u[b] * total;
-  if (threadIdx.x == block_pick<W>(before, mine, target, false, s.picks[1])) {
+  uint32_t who = block_pick<W>(before, mine, target, false, s.picks[1]);
+  if (who == kNone) {
+    if (threadIdx.x == 0) store_result(a, b, -1, 0.0f);
+    return;
+  }
+  if (threadIdx.x == who) {
     double rest = target - before;
     uint32_t at = q0;
 #pragma unroll 1
@@ -403,7 +410,8 @@ __device__ __forceinline__ void draw(const SampleArgs& a, int64_t b, const Row& 
   }
   double all;
   before = block_before<W>(mine, s.wave_f64[2], all);
-  if (threadIdx.x != block_pick<W>(before, mine, s.rest, false, s.picks[2])) return;
+  who = block_pick<W>(before, mine, s.rest, false, s.picks[2]);
+  if (threadIdx.x != (who == kNone ? 0 : who)) return;
   int32_t token = -1;
   float x = 0.0f;
 #pragma unroll 1
@@ -504,7 +512,7 @@ __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, 
         }
 #pragma unroll 1
         for (int i = threadIdx.x; i < kBins; i += W * kWave)
-          table[i] = i > 1 && i < kBins - 2 && i != kBinZero ? weight(bin_number(i)) : i == kBins - 2 ? __builtin_huge_val() : 0.0;
+          table[i] = i > kBinLow && i < kBinHigh && i != kBinZero ? weight(bin_number(i)) : i == kBinHigh ? __builtin_huge_val() : 0.0;
         __syncthreads();
         return true;
       },
@@ -718,6 +726,7 @@ __device__ __forceinline__ float fill_bins(const Row& r, uint32_t t0, uint32_t t
     __syncthreads();
   }
   float m = kMaskedRow;
+  bool any_low = false;
   stream_ring(r, t0 + wave, t1, W, [&](uint32_t t, u32x4 raw) {
     float y[E];
     tile_logits<DT>(r, t, raw, y);
@@ -742,7 +751,7 @@ __device__ __forceinline__ float fill_bins(const Row& r, uint32_t t0, uint32_t t
       } else {                              // masked logits would all wait for one counter
 #pragma unroll
         for (uint32_t j = 0; j < E; ++j)
-          if (y[j] > -kBinsBelow) atomicAdd(&count[bin_of(__builtin_bit_cast(uint32_t, y[j]))], 1u);
+          if (y[j] > kMaskedRow) atomicAdd(&count[bin_of(__builtin_bit_cast(uint32_t, y[j]))], 1u);
       }
       if (kOne && p > 0.0f && __builtin_amdgcn_ballot_w64(least < 0x1p-10f) != 0) {
 #pragma unroll 1
@@ -755,6 +764,7 @@ __device__ __forceinline__ float fill_bins(const Row& r, uint32_t t0, uint32_t t
     if (masses) {
 #pragma unroll
       for (uint32_t j = 0; j < E; ++j) {
+        any_low |= y[j] > kMaskedRow && !(y[j] > -kBinsBelow);
         if (!(y[j] > -kBinsBelow)) continue;
         const int bin = bin_of(__builtin_bit_cast(uint32_t, y[j]));
         const double rel = exp2_f64((double)(y[j] - bin_number(bin)) * r.c);
@@ -762,6 +772,7 @@ __device__ __forceinline__ float fill_bins(const Row& r, uint32_t t0, uint32_t t
       }
     }
   });
+  if (any_low) atomicAdd(&mass[kBinLow], (u64)1);  // that there are any is all that counts
   return m;
 }
 
@@ -830,18 +841,18 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
   // The bins must hold all logits that have a say, a bin's mass must fit (numbers of a bin differ by 2^-7 relative), and e^(x / T) of the
   // logits next to 0 must be a number.
   bool known = (k == 0 && p == 0.0f) ||
-               (top < kBinsBelow && (!masses || (double)top * r.inv_t < 300.0) && (p == 0.0f || r.inv_t < 300000.0) &&
-                (p == 0.0f || k > 0 || ((double)top + kBinsBelow) * r.inv_t > 50.0));
-  constexpr int kEach = (kBins - 2 + kThreads - 1) / kThreads;  // bins of a thread, from the top
-  const int highest = kBins - 2 - (int)threadIdx.x * kEach, lowest = max(highest - kEach + 1, 1);
+               (top < kBinsBelow && (!masses || (double)top * r.inv_t < 300.0) && (p == 0.0f || r.inv_t < 300000.0));
+  constexpr int kEach = (kBinHigh + kThreads - 1) / kThreads;  // bins of a thread, from the top
+  const int highest = kBinHigh - (int)threadIdx.x * kEach, lowest = max(highest - kEach + 1, kBinLow);
   int kbin = 0;                             // bins below it are out by top-k
+  bool ranked = false;                      // and it has been ranked for top-k: kept_mass is the mass of what is left of it
   if (known && k > 0) {
     uint32_t mine = 0, all;
 #pragma unroll 1
     for (int i = highest; i >= lowest; --i) mine += count[i];
     uint32_t before = block_before<W>(mine, s.wave_u32, all);
-    known = (uint32_t)k <= all;
-    if (known) {
+    uint32_t rank = all;                    // of the k-th largest among the members, from 1
+    if ((uint32_t)k <= all) {
       if (before < (uint32_t)k && (uint32_t)k <= before + mine) {
         int i = highest;
 #pragma unroll 1
@@ -855,31 +866,36 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
       }
       __syncthreads();
       kbin = (int)s.found_bin;
-      if (kOne && kbin != kBinZero) {
-        cut = bin_number(kbin);
-      } else {
-        const uint32_t rank = (uint32_t)k - (f.few ? 0 : s.above_count);  // among the members, from 1
-        known = collect_members<DT, W>(r, kbin, f.few, blocks, nblocks, members, s);
-        if (known) {
-          const uint32_t n = s.nmembers;
+      known = kbin != kBinLow;
+      rank = (uint32_t)k - (f.few ? 0 : s.above_count);
+      ranked = known && !(kOne && kbin != kBinZero);
+      if (known && !ranked) cut = bin_number(kbin);
+    } else if (f.few) {                     // fewer logits than k: they are all members
+      known = count[kBinLow] == 0;
+      kbin = kBinLow + 1;
+      ranked = known;
+    }
+    if (ranked) {
+      ranked = known = collect_members<DT, W>(r, kbin, f.few, blocks, nblocks, members, s);
+      if (known) {
+        const uint32_t n = s.nmembers;
+        if (threadIdx.x == 0) s.kept_mass = 0;
 #pragma unroll 1
-          for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-            uint32_t above = 0, level = 0;
-            const float mine = members[i];
+        for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+          uint32_t above = 0, level = 0;
+          const float mine = members[i];
 #pragma unroll 8
-            for (uint32_t j = 0; j < n; ++j) above += members[j] > mine, level += members[j] == mine;
-            if (above < rank && rank <= above + level) s.cut_key = __builtin_bit_cast(uint32_t, members[i]);
-          }
-          if (threadIdx.x == 0) s.kept_mass = 0;
-          __syncthreads();
-          cut = __builtin_bit_cast(float, s.cut_key);
-          if (p > 0.0f) {
-#pragma unroll 1
-            for (uint32_t i = threadIdx.x; i < n; i += kThreads)
-              if (members[i] >= cut) atomicAdd(&s.kept_mass, fixed_point(r.weight(members[i]), kFixed));
-          }
-          __syncthreads();
+          for (uint32_t j = 0; j < n; ++j) above += members[j] > mine, level += members[j] == mine;
+          if (above < rank && rank <= above + level) s.cut_key = __builtin_bit_cast(uint32_t, mine);
         }
+        __syncthreads();
+        cut = __builtin_bit_cast(float, s.cut_key);
+        if (p > 0.0f) {
+#pragma unroll 1
+          for (uint32_t i = threadIdx.x; i < n; i += kThreads)
+            if (members[i] >= cut) atomicAdd(&s.kept_mass, fixed_point(r.weight(members[i]), kFixed));
+        }
+        __syncthreads();
       }
     }
   }
@@ -889,12 +905,15 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
     rank_mass = true;
     target = (double)p * (double)s.kept_mass * (1.0 / kFixed);
   } else if (known && p > 0.0f) {
+    // logits of -128 and less: there are none, or top-k leaves none, or they weigh nothing
+    known = kbin > kBinLow || ((double)top + kBinsBelow) * r.inv_t > 50.0 || (kOne ? count[kBinLow] == 0 : mass[kBinLow] == 0);
+  }
+  if (known && p > 0.0f && !f.few) {
     double zero = 0.0;
     if constexpr (kOne) {
       block_before<W>(next_to_0, s.wave_f64[1], zero);
       zero *= exp2_f64(-r.m * r.c);
     }
-    const bool ranked = k > 0 && !(kOne && kbin != kBinZero);  // bin kbin has been ranked for top-k
     const auto bin_mass = [&](int bin) {
       double n = kOne ? (double)count[bin] : (double)mass[bin] * (1.0 / kBinMass);
       n *= r.weight(bin_number(bin));
@@ -936,7 +955,7 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
       cut = bin_number(bin);
     } else {
       rank_mass = true;
-      if (bin != kbin || k == 0) known = collect_members<DT, W>(r, bin, false, blocks, nblocks, members, s);
+      if (!ranked || bin != kbin) known = collect_members<DT, W>(r, bin, false, blocks, nblocks, members, s);
     }
   }
   if (known && rank_mass) {
@@ -1052,6 +1071,7 @@ __global__ __launch_bounds__(W* kWave) void espo_sample_kernel(SampleArgs a) {
   }
   if constexpr (kFilters) {
     if (!w.is_plain()) {
+      if (threadIdx.x == 0) s.found_bin = 0;  // where NaN leaves nothing to be found
       draw_filtered<DT, W, kJoin>(a, b, r, w.f, lds, s);
       return;
     }

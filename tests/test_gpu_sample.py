@@ -170,6 +170,73 @@ def test_wide_and_shifted_logits(dtype):
         run(x, u, **mode)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V,left", [(4099, 7), (4099, 350), (40001, 900), (40001, 1)])
+def test_filters_over_fewer_logits_than_top_k(V, left, dtype):
+    """A grammar's mask leaves `left` logits: a top-k beyond that is no filter, and the nucleus is of what is left."""
+    print(f"[case] sample mask leaves {left} of {V} {dtype}", flush=True)
+    x, g = logits(5, V, dtype, seed=left)
+    for b in range(5):
+        out = torch.randperm(V, generator=g)[left:].cuda()
+        x[b, out] = [-math.inf, torch.finfo(dtype).min, -1e30][b % 3]
+    u = torch.rand(5, generator=g)
+    for k in (left, left + 1, left + 40, V - 1):
+        run(x, u, k=k)
+        run(x, u, T=0.8, k=k, p=0.9)
+        run(x, u, k=k, min_p=0.05)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [1.0, 4.0, 9.0])
+def test_filters_around_128(T, dtype):
+    print(f"[case] sample around 128, T={T} {dtype}", flush=True)
+    x, g = logits(6, 5003, dtype, seed=31)
+    x[0, ::2] = -128.0
+    x[1, ::3] = -130.0 - torch.rand(1668, generator=g).to(dtype).cuda() * 20
+    x[2] -= 300.0                                              # all of it beyond
+    x[3, :40] += 135.0                                         # the maximum beyond on the other side
+    x[4, ::2] = torch.linspace(-160, 100, 2502).to(dtype).cuda()
+    x[5, 10:] = -200.0
+    u = torch.rand(6, generator=g)
+    for mode in (dict(k=5), dict(k=4000), dict(k=4000, p=0.99), dict(p=0.9), dict(p=0.9999), dict(k=300, p=0.8, min_p=0.01)):
+        run(x, u, T=T, **mode)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_longest_rows(dtype):
+    print(f"[case] sample longest rows {dtype}", flush=True)
+    for V, modes in ((1 << 19, (dict(), dict(k=60, p=0.9), dict(p=0.8), dict(T=3.0, k=30000, min_p=1e-4))), (1 << 20, (dict(), dict(T=0.4), dict(T=0.0)))):
+        x, g = logits(2, V, dtype, seed=V % 1000)
+        for mode in modes:
+            run(x, torch.rand(2, generator=g), **mode)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_with_nan_leave_the_others_alone(dtype):
+    print(f"[case] sample rows with NaN and +inf {dtype}", flush=True)
+    for B, V in ((12, 3001), (8, 152064)):
+        x, g = logits(B, V, dtype, seed=51)
+        x[1] = math.nan
+        x[3, ::2] = math.nan
+        x[4, 77] = math.inf
+        x[6, V - 1] = -math.nan
+        bad = torch.tensor([1, 3, 4, 6])
+        good = torch.tensor([b for b in range(B) if b not in (1, 3, 4, 6)])
+        u = torch.rand(B, generator=g)
+        for mode in (dict(), dict(top_k=7), dict(top_p=0.7), dict(min_p=0.1), dict(top_k=50, top_p=0.9), dict(top_k=2900)):
+            s = {k: torch.full((B,), v, device="cuda", dtype=torch.int32 if k == "top_k" else F32) for k, v in mode.items()}
+            n = espo.espo_sample_workspace_bytes(B, V, dtype)
+            ws = torch.zeros(n, dtype=torch.uint8, device="cuda") if n else None
+            tokens = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+            espo.espo_sample(x, u.cuda(), tokens, workspace=ws, **s)
+            alive = torch.ones(B, dtype=torch.uint8)
+            alive[bad] = 0
+            alone = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+            espo.espo_sample(x, u.cuda(), alone, alive=alive.cuda(), **s)
+            assert torch.equal(tokens[good.cuda()], alone[good.cuda()]) and (alone[good.cuda()] >= 0).all()
+            assert ((tokens[bad.cuda()] >= -1) & (tokens[bad.cuda()] < V)).all()
+
+
 def test_frequencies_are_the_distribution():
     print("[case] sample frequencies", flush=True)
     n, V = 4096, 300
