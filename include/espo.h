@@ -505,7 +505,7 @@ int espo_length_order(const int32_t* lengths, int64_t B, int64_t T, int32_t* ord
  *
  * Arguments
  *   logits      device, [B, row_stride] elements of `dt`, base and row pitch in bytes multiples of 16, as for espo_step.
- *   B, V        B >= 0 (0 is a no-op), V >= 1; B < 2^31, V <= 2^20, with any filter given V <= 2^19 (ESPO_ERANGE).
+ *   B, V        B >= 0 (0 is a no-op), V >= 1; B < 2^23, V <= 2^20, with any filter given V <= 2^19 (ESPO_ERANGE).
  *   row_stride  elements between rows, >= V.
  *   temperature, top_p, min_p   device, [B] fp32;  top_k  device, [B] int32.  Each may be NULL: temperature 1, that filter off.
  *   u           device, [B] fp32.
@@ -522,7 +522,7 @@ int espo_sample(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_t
                 const int32_t* top_k, const float* top_p, const float* min_p, const float* u, const uint8_t* alive,
                 int32_t* tokens, float* logprob, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace for espo_sample (0 where it needs none). */
+/* Bytes of workspace with which espo_sample splits the rows of this shape (0 where it does not). */
 size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
 
 /*
@@ -542,7 +542,7 @@ size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
  *
  * Arguments
  *   logits      device, [N, row_stride] elements of `dt`, base and row pitch in bytes multiples of 16, as for espo_step.
- *   N, V        N >= 0 (0 is a no-op), V >= 1; N < 2^31, V <= 2^30, and for the gradient N * ceil(V / 8192) < 2^31
+ *   N, V        N >= 0 (0 is a no-op), V >= 1; N < 2^23, V <= 2^30, and for the gradient N * ceil(V / 8192) < 2^24
  *               (bf16; V / 4096 for fp32) (ESPO_ERANGE).
  *   row_stride  elements between rows, >= V.
  *   temperature between 1e-6 and 1e26.
@@ -553,7 +553,12 @@ size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
  *   stats       device, [N][2] fp32 out, 8-byte aligned, may be NULL: max x and S of every row, for espo_logprobs_backward.
  *   dlogprob    device, [N] fp32;  dentropy  device, [N] fp32 or NULL.
  *   dlogits     device, [N, grad_stride] of `dt`, base and row pitch multiples of 16 bytes; only the first V of each row are written.
- *               May be `logits` itself with grad_stride = row_stride (the gradient then replaces the logits); no other overlap.
+ *               May be `logits` itself with grad_stride = row_stride (the gradient then replaces the logits).  No other output may
+ *               overlap an input.
+ *   workspace   optional device scratch of at least espo_logprobs_workspace_bytes(N, V, dt) bytes, 16-byte aligned, with which
+ *               long rows are split over several workgroups where there are few.  Without it (NULL, too short or misaligned), and
+ *               where that size is 0, one workgroup handles a whole row.  What it holds before and after the call does not matter; calls
+ *               that may run at the same time need a workspace each.
  *   stream      hipStream_t as void*.
  */
 int espo_logprobs(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
@@ -564,7 +569,7 @@ int espo_logprobs_backward(const void* logits, espo_dtype dt, int64_t N, int64_t
                            const int32_t* tokens, const float* stats, const float* entropy,
                            const float* dlogprob, const float* dentropy, void* dlogits, int64_t grad_stride, void* stream);
 
-/* Bytes of workspace for espo_logprobs (0 where it needs none). */
+/* Bytes of workspace with which espo_logprobs splits the rows of this shape (0 where it does not). */
 size_t espo_logprobs_workspace_bytes(int64_t N, int64_t V, espo_dtype dt);
 
 /*

@@ -122,7 +122,7 @@ int rows_checked(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_
   if (!(temperature >= 1e-6f && temperature <= 1e26f)) return ESPO_EINVAL;  // a logit over T stays an fp32 number, and -1e30 over T far from 0
   if (N == 0) return ESPO_OK;
   if (!logits || !tokens) return ESPO_EINVAL;
-  if (N > 0x7fffffff || V > (1 << 30)) return ESPO_ERANGE;
+  if (N >= (1 << 23) || V > (1 << 30)) return ESPO_ERANGE;  // a launch has fewer than 2^32 threads, 512 a row
   if (!aligned16(logits) || ((size_t)row_stride * (dt == ESPO_BF16 ? 2 : 4)) % 16 != 0) return ESPO_EALIGN;
   return ESPO_OK;
 }
@@ -404,26 +404,27 @@ int espo_sample(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_t
   if (B < 0 || V < 1 || row_stride < V) return ESPO_EINVAL;
   if (B == 0) return ESPO_OK;
   if (!logits || !u || !tokens) return ESPO_EINVAL;
-  if (B > 0x7fffffff || V > (top_k || top_p || min_p ? 1 << 19 : 1 << 20)) return ESPO_ERANGE;  // a filter keeps the maxima of blocks in LDS
+  if (B >= (1 << 23) || V > (top_k || top_p || min_p ? 1 << 19 : 1 << 20)) return ESPO_ERANGE;  // a filter keeps the maxima of blocks in LDS
   if (!aligned16(logits) || ((size_t)row_stride * (dt == ESPO_BF16 ? 2 : 4)) % 16 != 0) return ESPO_EALIGN;
   return espo::launch_sample(logits, dt, B, V, row_stride, temperature, top_k, top_p, min_p, u, alive, tokens, logprob,
                              workspace, workspace_bytes, (hipStream_t)stream);
 }
 
 size_t espo_logprobs_workspace_bytes(int64_t N, int64_t V, espo_dtype dt) {
-  (void)N; (void)V; (void)dt;
-  return 0;
+  if (N <= 0 || N >= (1 << 23) || V < 1 || V > (1 << 30) || (dt != ESPO_F32 && dt != ESPO_BF16)) return 0;
+  return espo::logprobs_workspace(dt, N, V);
 }
 
 int espo_logprobs(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
                   const int32_t* tokens, float* logprob, float* entropy, float* stats, void* workspace, size_t workspace_bytes,
                   void* stream) {
-  (void)workspace; (void)workspace_bytes;
   const int rc = rows_checked(logits, dt, N, V, row_stride, temperature, tokens);
   if (rc != ESPO_OK || N == 0) return rc;
   if (!logprob) return ESPO_EINVAL;
   if (((uintptr_t)stats & 7u) != 0) return ESPO_EALIGN;
-  return espo::launch_logprobs(logits, dt, N, V, row_stride, temperature, tokens, logprob, entropy, stats, (hipStream_t)stream);
+  // the split is an offer: without a workspace that fits, one workgroup handles a whole row
+  if (!workspace || workspace_bytes < espo::logprobs_workspace(dt, N, V) || !aligned16(workspace)) workspace = nullptr;
+  return espo::launch_logprobs(logits, dt, N, V, row_stride, temperature, tokens, logprob, entropy, stats, workspace, (hipStream_t)stream);
 }
 
 int espo_logprobs_backward(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
@@ -440,8 +441,8 @@ int espo_logprobs_backward(const void* logits, espo_dtype dt, int64_t N, int64_t
 }
 
 size_t espo_policy_loss_workspace_bytes(int64_t N, int64_t V, espo_dtype dt) {
-  if (N <= 0 || V < 1 || (dt != ESPO_F32 && dt != ESPO_BF16)) return 0;
-  return espo::policy_workspace(N);
+  if (N <= 0 || N >= (1 << 23) || V < 1 || V > (1 << 30) || (dt != ESPO_F32 && dt != ESPO_BF16)) return 0;
+  return espo::policy_workspace(dt, N, V);
 }
 
 int espo_policy_loss(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature,
@@ -459,7 +460,7 @@ int espo_policy_loss(const void* logits, espo_dtype dt, int64_t N, int64_t V, in
     if (rc != ESPO_OK) return rc;
   }
   if (((uintptr_t)out & 7u) != 0) return ESPO_EALIGN;
-  if (N > 0 && (!workspace || workspace_bytes < espo::policy_workspace(N) || !aligned16(workspace))) return ESPO_EWORKSPACE;
+  if (N > 0 && (!workspace || workspace_bytes < espo::policy_workspace(dt, N, V) || !aligned16(workspace))) return ESPO_EWORKSPACE;
   return espo::launch_policy_loss(logits, dt, N, V, row_stride, temperature, tokens, old_logprob, adv, weights, *ctrl, dlogits,
                                   grad_stride, logprob, entropy, out, workspace, (hipStream_t)stream);
 }

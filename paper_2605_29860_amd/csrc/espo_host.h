@@ -86,13 +86,15 @@ size_t sample_workspace(int dt, int64_t B, int64_t V);
 
 // The policy update's operators.  stats: [N] pairs of row maximum and sum.
 int launch_logprobs(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,
-                    float* logprob, float* entropy, float* stats, hipStream_t stream);
+                    float* logprob, float* entropy, float* stats, void* workspace, hipStream_t stream);
+// Bytes with which the forward pass over few rows is split over several workgroups each, 0 where it is not.
+size_t logprobs_workspace(int dt, int64_t N, int64_t V);
 int launch_logprobs_backward(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,
                              const float* stats, const float* entropy, const float* dlogprob, const float* dentropy, void* dlogits,
                              int64_t grad_stride, hipStream_t stream);
 // Whether the gradient's grid fits the index of a launch.
 bool grad_indexable(int dt, int64_t N, int64_t V);
-size_t policy_workspace(int64_t N);
+size_t policy_workspace(int dt, int64_t N, int64_t V);
 int launch_policy_loss(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,
                        const float* old_logprob, const float* adv, const float* weights, const espo_policy_ctrl& c, void* dlogits,
                        int64_t grad_stride, float* logprob, float* entropy, espo_policy_result* out, void* workspace, hipStream_t stream);

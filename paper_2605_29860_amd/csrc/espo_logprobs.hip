@@ -20,7 +20,7 @@ namespace {
 constexpr int kRowWaves = 8, kRowThreads = kRowWaves * kWave;
 constexpr int kGradThreads = 256, kGradLoads = 4;
 constexpr int kGradSpan = kGradThreads * kGradLoads;  // vectors of a workgroup
-constexpr int kComputeUnits = 256;
+constexpr int kComputeUnits = 256, kMostParts = 16;
 // Rows are held by a workgroup each from this many waves on (the chip has 4096 at a time); fewer leave compute units idle, and two passes of
 // smaller workgroups are faster.  us, held / two passes: V = 152064 bf16 (16 waves) N = 64 30.9 / 25.8, 96 31.4 / 30.4, 128 32.1 / 34.9,
 // 256 37.6 / 46.9; V = 32768 f32 (8 waves) N = 160 17.7 / 18.0, 256 19.0 / 24.4; V = 32000 bf16 (4 waves) N = 256 17.7 / 16.3, 512 21.5 / 24.7.
@@ -58,25 +58,16 @@ __device__ __forceinline__ void store_row(const RowOutputs& o, int64_t row, floa
   if (o.stats) o.stats[row] = stats;
 }
 
-// One workgroup per row, which is read once.
+// The sums of tiles t0 .. t1 - 1 of a row, the same in every thread.
 template <int DT, bool kEntropy>
-__global__ __launch_bounds__(kRowThreads) void espo_logprobs_kernel(RowArgs a, RowOutputs o) {
-  __shared__ SoftmaxSums lds[kRowWaves];
+__device__ __forceinline__ SoftmaxSums sum_tiles(const RowArgs& a, const RowView& r, uint32_t t0, uint32_t t1, SoftmaxSums* lds) {
   constexpr int E = vec_elems<DT>();
-  const int64_t row = blockIdx.x;
-  const int32_t token = a.tokens[row];
-  if (!used_row(token, a.V)) {
-    if (threadIdx.x == 0) store_row(o, row, 0.0f, 0.0f, float2{0.0f, 1.0f});
-    return;
-  }
-  const char* x = a.logits + row * a.row_bytes;
-  const RowView r = row_view<DT>(x, a.V);
   SoftmaxSums p = kNoSums;
-  stream_tiles(r, threadIdx.x >> 6, r.ntiles, kRowWaves, [&](uint32_t t, const u32x4* raw) {
+  stream_tiles(r, t0 + (threadIdx.x >> 6), t1, kRowWaves, [&](uint32_t t, const u32x4* raw) {
     float y[kAhead][E], m = p.m;
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      if (t + j * kRowWaves >= r.ntiles) {
+      if (t + j * kRowWaves >= t1) {
 #pragma unroll
         for (int i = 0; i < E; ++i) y[j][i] = kNegInf;
         continue;
@@ -88,18 +79,54 @@ __global__ __launch_bounds__(kRowThreads) void espo_logprobs_kernel(RowArgs a, R
     follow<kEntropy>(p, m, a.k2);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
-      if (t + j * kRowWaves < r.ntiles) {
+      if (t + j * kRowWaves < t1) {
 #pragma unroll
         for (int i = 0; i < E; ++i) add_logit<kEntropy>(p, y[j][i], a.k2);
       }
   });
-  p = block_merge<kRowWaves, kEntropy>(p, a.k2, lds);
-  if (threadIdx.x == 0) {
-    float logprob, entropy;
-    float2 stats;
-    row_results(a, logit_at<DT>(x, (uint32_t)token), p, logprob, entropy, stats);
-    store_row(o, row, logprob, entropy, stats);
+  return block_merge<kRowWaves, kEntropy>(p, a.k2, lds);
+}
+
+// One workgroup per row, which is read once; or, where there are few rows, `parts` workgroups that leave their sums for
+// espo_logprobs_join_kernel.
+template <int DT, bool kEntropy, bool kSplit>
+__global__ __launch_bounds__(kRowThreads) void espo_logprobs_kernel(RowArgs a, RowOutputs o, SoftmaxSums* split, uint32_t parts) {
+  __shared__ SoftmaxSums lds[kRowWaves];
+  const int64_t row = kSplit ? blockIdx.x / parts : blockIdx.x;
+  const int32_t token = a.tokens[row];
+  if (!used_row(token, a.V)) {
+    if (!kSplit && threadIdx.x == 0) store_row(o, row, 0.0f, 0.0f, float2{0.0f, 1.0f});
+    return;
   }
+  const char* x = a.logits + row * a.row_bytes;
+  const RowView r = row_view<DT>(x, a.V);
+  if constexpr (kSplit) {
+    const uint32_t part = blockIdx.x % parts, each = (r.ntiles + parts - 1) / parts, t0 = part * each;
+    const SoftmaxSums p = sum_tiles<DT, kEntropy>(a, r, t0, min(t0 + each, r.ntiles), lds);
+    if (threadIdx.x == 0) split[blockIdx.x] = p;
+  } else {
+    const SoftmaxSums p = sum_tiles<DT, kEntropy>(a, r, 0, r.ntiles, lds);
+    if (threadIdx.x == 0) {
+      float logprob, entropy;
+      float2 stats;
+      row_results(a, logit_at<DT>(x, (uint32_t)token), p, logprob, entropy, stats);
+      store_row(o, row, logprob, entropy, stats);
+    }
+  }
+}
+
+// The parts' sums of a row put together, by a wave.
+template <int DT, bool kEntropy>
+__global__ __launch_bounds__(kWave) void espo_logprobs_join_kernel(RowArgs a, RowOutputs o, const SoftmaxSums* split, uint32_t parts) {
+  const int64_t row = blockIdx.x;
+  const int32_t token = a.tokens[row];
+  float logprob = 0.0f, entropy = 0.0f;
+  float2 stats{0.0f, 1.0f};
+  if (used_row(token, a.V)) {
+    const SoftmaxSums p = wave_merge<kEntropy>(threadIdx.x < parts ? split[row * parts + threadIdx.x] : kNoSums, a.k2);
+    row_results(a, logit_at<DT>(a.logits + row * a.row_bytes, (uint32_t)token), p, logprob, entropy, stats);
+  }
+  if (threadIdx.x == 0) store_row(o, row, logprob, entropy, stats);
 }
 
 // The objective at one token: L = s w (-min(r A, clip(r) A) - c H) with r = exp(ln pi - ln pi_old).
@@ -419,12 +446,33 @@ RowArgs row_args(const void* logits, int dt, int64_t N, int64_t V, int64_t row_s
                  (float)(1.4426950408889634 / (double)temperature), tokens};
 }
 
+// Workgroups that a row of few is split over: what two per compute unit allow, of at least 32 tiles each (four per wave), and at least 8,
+// because the second launch costs 2 to 3 us.  (With the entropy, us, whole and split: bf16 V = 152064 N = 1 12.6 and 5.3, N = 64 13.3 and 9.0,
+// N = 100, over 5, 13.6 and 10.2, all without the host's time; fp32 V = 65536 N = 32 8.2 and 5.6; bf16 V = 65536, over 4, 7.2 and 6.0.)
+uint32_t forward_parts(int dt, int64_t N, int64_t V) {
+  const int64_t tiles = V / (kWave * (dt == ESPO_BF16 ? 8 : 4));
+  int64_t n = 2 * kComputeUnits / N;
+  if (n > tiles / 32) n = tiles / 32;
+  if (n > kMostParts) n = kMostParts;
+  return n < 8 ? 1u : (uint32_t)n;
+}
+
+template <int DT, bool kEntropy>
+void forward(const RowArgs& a, const RowOutputs& o, SoftmaxSums* split, hipStream_t stream) {
+  const uint32_t parts = split ? forward_parts(DT, a.N, a.V) : 1;
+  if (parts > 1) {
+    hipLaunchKernelGGL((espo_logprobs_kernel<DT, kEntropy, true>), dim3((unsigned)(a.N * parts)), dim3(kRowThreads), 0, stream, a, o, split, parts);
+    hipLaunchKernelGGL((espo_logprobs_join_kernel<DT, kEntropy>), dim3((unsigned)a.N), dim3(kWave), 0, stream, a, o, split, parts);
+  } else {
+    hipLaunchKernelGGL((espo_logprobs_kernel<DT, kEntropy, false>), dim3((unsigned)a.N), dim3(kRowThreads), 0, stream, a, o, nullptr, 1u);
+  }
+}
 template <int DT>
-void forward(const RowArgs& a, const RowOutputs& o, hipStream_t stream) {
+void forward(const RowArgs& a, const RowOutputs& o, SoftmaxSums* split, hipStream_t stream) {
   if (o.entropy)
-    hipLaunchKernelGGL((espo_logprobs_kernel<DT, true>), dim3((unsigned)a.N), dim3(kRowThreads), 0, stream, a, o);
+    forward<DT, true>(a, o, split, stream);
   else
-    hipLaunchKernelGGL((espo_logprobs_kernel<DT, false>), dim3((unsigned)a.N), dim3(kRowThreads), 0, stream, a, o);
+    forward<DT, false>(a, o, split, stream);
 }
 
 template <int DT, bool kPolicy>
@@ -471,14 +519,14 @@ void policy_held(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const
 
 // Log-probabilities, entropy and, if it is wanted, the gradient of the objective.
 template <int DT>
-void policy(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, hipStream_t stream) {
+void policy(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, SoftmaxSums* split, hipStream_t stream) {
   const int waves = d.dlogits ? held_waves<DT>(a.V) : 0;
   switch (a.N * waves >= kHeldWaves ? waves : 0) {
     case 4: return policy_held<DT, 4>(a, o, d, q, stream);
     case 8: return policy_held<DT, 8>(a, o, d, q, stream);
     case 16: return policy_held<DT, 16>(a, o, d, q, stream);
   }
-  forward<DT>(a, o, stream);
+  forward<DT>(a, o, split, stream);
   if (d.dlogits) backward<DT, true>(a, d, q, stream);
 }
 
@@ -491,15 +539,21 @@ int launched() { return hipGetLastError() == hipSuccess ? ESPO_OK : ESPO_EHIP; }
 
 }  // namespace
 
-bool grad_indexable(int dt, int64_t N, int64_t V) { return N * (int64_t)grad_spans(dt, V) <= 0x7fffffff; }
+// (A launch has fewer than 2^32 threads.)
+bool grad_indexable(int dt, int64_t N, int64_t V) { return N * (int64_t)grad_spans(dt, V) < ((int64_t)1 << 32) / kGradThreads; }
 
 int launch_logprobs(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,
-                    float* logprob, float* entropy, float* stats, hipStream_t stream) {
+                    float* logprob, float* entropy, float* stats, void* workspace, hipStream_t stream) {
   const RowArgs a = row_args(logits, dt, N, V, row_stride, temperature, tokens);
   const RowOutputs o{logprob, entropy, (float2*)stats};
-  if (dt == ESPO_BF16) forward<ESPO_BF16>(a, o, stream);
-  else forward<ESPO_F32>(a, o, stream);
+  if (dt == ESPO_BF16) forward<ESPO_BF16>(a, o, (SoftmaxSums*)workspace, stream);
+  else forward<ESPO_F32>(a, o, (SoftmaxSums*)workspace, stream);
   return launched();
+}
+
+size_t logprobs_workspace(int dt, int64_t N, int64_t V) {
+  const uint32_t parts = forward_parts(dt, N, V);
+  return parts > 1 ? (size_t)N * parts * sizeof(SoftmaxSums) : 0;
 }
 
 int launch_logprobs_backward(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,
@@ -512,8 +566,8 @@ int launch_logprobs_backward(const void* logits, int dt, int64_t N, int64_t V, i
   return launched();
 }
 
-// Per row: maximum and sum, log-probability, entropy.
-size_t policy_workspace(int64_t N) { return (size_t)N * 16; }
+// Per row: maximum and sum, log-probability, entropy; behind them what the forward pass needs.
+size_t policy_workspace(int dt, int64_t N, int64_t V) { return (size_t)N * 16 + logprobs_workspace(dt, N, V); }
 
 int launch_policy_loss(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,
                        const float* old_logprob, const float* adv, const float* weights, const espo_policy_ctrl& c, void* dlogits,
@@ -526,8 +580,9 @@ int launch_policy_loss(const void* logits, int dt, int64_t N, int64_t V, int64_t
   const RowOutputs o{logprob, entropy, stats};
   const GradArgs d{(char*)dlogits, grad_stride * (dt == ESPO_BF16 ? 2 : 4), grad_spans(dt, V), stats, entropy, nullptr, nullptr, logprob};
   if (N > 0) {
-    if (dt == ESPO_BF16) policy<ESPO_BF16>(a, o, d, q, stream);
-    else policy<ESPO_F32>(a, o, d, q, stream);
+    SoftmaxSums* split = (SoftmaxSums*)(stats + 2 * N);
+    if (dt == ESPO_BF16) policy<ESPO_BF16>(a, o, d, q, split, stream);
+    else policy<ESPO_F32>(a, o, d, q, split, stream);
     if (launched() != ESPO_OK) return ESPO_EHIP;
   }
   hipLaunchKernelGGL(espo_policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, stream, tokens, logprob, entropy, N, (uint32_t)V, q, out);

@@ -333,3 +333,30 @@ def test_row_offsets_beyond_32_bits():
     espo.espo_logprobs_backward(small, 1.0, tokens, stats, w, d)
     espo.espo_logprobs_backward(x, 1.0, tokens, stats, w, x)
     assert torch.equal(x.float(), d.float())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_few_long_rows_split_with_a_workspace(dtype):
+    for N, V in ((1, 152064), (3, 140001), (32, 152064), (60, 131072), (5, 1 << 20)):
+        print(f"[case] logprobs split N={N} V={V} {dtype}", flush=True)
+        x, tokens, x64, _, _ = make(N, V, dtype, seed=N + V, masked=0.1, pad=5)
+        tokens[0] = V - 1
+        if N > 1:
+            tokens[N // 2] = -1
+        n = espo.espo_logprobs_workspace_bytes(N, V, dtype)
+        assert n > 0
+        ws = torch.full((n + 16,), 0xFF, dtype=torch.uint8, device="cuda")
+        out = lambda: [torch.full((N,), math.nan, device="cuda") for _ in range(2)] + [torch.full((2 * N,), math.nan, device="cuda")]
+        whole, split, offset = out(), out(), out()
+        espo.espo_logprobs(x, 0.8, tokens, whole[0], entropy=whole[1], stats=whole[2])
+        espo.espo_logprobs(x, 0.8, tokens, split[0], entropy=split[1], stats=split[2], workspace=ws[:n])
+        espo.espo_logprobs(x, 0.8, tokens, offset[0], entropy=offset[1], stats=offset[2], workspace=ws[4:])   # misaligned: not used
+        assert all(torch.equal(a, b) for a, b in zip(whole, offset)) and (ws[n:] == 0xFF).all()
+        f = R.softmax_rows(x64, 0.8, tokens.cpu())
+        for got in (whole, split):
+            check(got[0], f["logprob"], R.logprob_bound(f, V), "logprob")
+            check(got[1], f["entropy"], R.entropy_bound(f, V), "entropy")
+        assert torch.equal(whole[2][0::2], split[2][0::2])     # the maximum is the same number
+        alone = torch.full((N,), math.nan, device="cuda")
+        espo.espo_logprobs(x, 0.8, tokens, alone, workspace=ws)
+        check(alone, f["logprob"], R.logprob_bound(f, V), "logprob without the entropy")

@@ -28,7 +28,7 @@ def test_sample_refusals(lib):
     assert call(dt=2) == -1 and call(B=-1) == -1 and call(V=0) == -1 and call(stride=63) == -1
     assert call(logits=None) == -1 and call(u=None) == -1 and call(tokens=None) == -1
     assert call(logits=ODD) == -2 and call(V=63, stride=63) == -2
-    assert call(B=1 << 31) == -5 and call(V=(1 << 20) + 1, stride=1 << 21) == -5
+    assert call(B=1 << 31) == -5 and call(B=1 << 23) == -5 and call(V=(1 << 20) + 1, stride=1 << 21) == -5
     for name in ("k", "p", "min_p"):
         assert call(V=(1 << 19) + 1, stride=1 << 21, **{name: FAKE}) == -5
 
@@ -42,7 +42,7 @@ def test_logprobs_refusals(lib):
         assert call(T=T) == -1, T
     assert call(logits=None) == -1 and call(tokens=None) == -1 and call(lp=None) == -1
     assert call(logits=ODD) == -2 and call(V=63, stride=63) == -2 and call(stats=ODD) == -2
-    assert call(N=1 << 31) == -5 and call(V=(1 << 30) + 1, stride=1 << 31) == -5
+    assert call(N=1 << 31) == -5 and call(N=1 << 23) == -5 and call(V=(1 << 30) + 1, stride=1 << 31) == -5
 
 
 def test_logprobs_backward_refusals(lib):
@@ -55,6 +55,21 @@ def test_logprobs_backward_refusals(lib):
     assert call(d=ODD) == -2 and call(ds=65) == -2 and call(stats=ODD) == -2
     big = lambda N: lib.espo_logprobs_backward(FAKE, 1, N, 8193, 8200, 1.0, FAKE, FAKE, None, FAKE, None, C.c_void_p(0x2000), 8200, None)
     assert big(1 << 30) == -5                                # two workgroups a row
+
+
+def test_launches_that_would_not_fit_are_refused(lib):
+    # one workgroup of 256 threads per 8192 logits in bf16, per 4096 in fp32; a launch has fewer than 2^32 threads
+    grad = lambda dt, N, V: lib.espo_logprobs_backward(FAKE, dt, N, V, V, 1.0, FAKE, FAKE, None, FAKE, None, C.c_void_p(0x2000), V, None)
+    assert grad(1, 1 << 22, 4 * 8192) == -5 and grad(0, 1 << 22, 4 * 4096) == -5 and grad(1, 1 << 23, 8) == -5
+    assert lib.espo_logprobs_workspace_bytes(1 << 23, 152064, 1) == 0 and lib.espo_policy_loss_workspace_bytes(1 << 23, 152064, 1) == 0
+
+
+def test_shapes_that_are_split_ask_for_a_workspace(lib):
+    for fn in (lib.espo_sample_workspace_bytes, lib.espo_logprobs_workspace_bytes):
+        for dt in (0, 1):
+            assert fn(8, 152064, dt) > 0                       # few long rows: most compute units would idle
+            assert fn(512, 152064, dt) == 0 and fn(8, 1000, dt) == 0 and fn(0, 152064, dt) == 0 and fn(8, 0, dt) == 0
+            assert fn(8, 152064, 7) == 0
 
 
 def test_policy_loss_refusals(lib):
