@@ -542,7 +542,7 @@ size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
  *
  * Arguments
  *   logits      device, [N, row_stride] elements of `dt`, base and row pitch in bytes multiples of 16, as for espo_step.
- *   N, V        N >= 0 (0 is a no-op), V >= 1; N < 2^23, V <= 2^30, and for the gradient N * ceil(V / 8192) < 2^24
+ *   N, V        N >= 0 (0 is a no-op), V >= 1; N < 2^23, V <= 2^30, and for the gradient N * ceil(V / 8192) < 2^24 - 1
  *               (bf16; V / 4096 for fp32) (ESPO_ERANGE).
  *   row_stride  elements between rows, >= V.
  *   temperature between 1e-6 and 1e26.

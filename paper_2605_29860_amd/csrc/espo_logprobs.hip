@@ -22,9 +22,9 @@ constexpr int kGradThreads = 256, kGradLoads = 4;
 constexpr int kGradSpan = kGradThreads * kGradLoads;  // vectors of a workgroup
 constexpr int kComputeUnits = 256, kMostParts = 16;
 // Rows are held by a workgroup each from this many waves on (the chip has 4096 at a time); fewer leave compute units idle, and two passes of
-// smaller workgroups are faster.  us, held / two passes: V = 152064 bf16 (16 waves) N = 64 30.9 / 25.8, 96 31.4 / 30.4, 128 32.1 / 34.9,
-// 256 37.6 / 46.9; V = 32768 f32 (8 waves) N = 160 17.7 / 18.0, 256 19.0 / 24.4; V = 32000 bf16 (4 waves) N = 256 17.7 / 16.3, 512 21.5 / 24.7.
-constexpr int64_t kHeldWaves = 1600;
+// smaller workgroups are faster.  us, held / two passes: V = 152064 bf16 (16 waves) N = 64 29.7 / 16.1, 128 31.5 / 30.2, 160 32.2 / 33.2,
+// 256 39.8 / 45.1; V = 70000 bf16 (8 waves) N = 200 22.5 / 21.1, 256 23.7 / 24.5; V = 32000 bf16 (4 waves) N = 400 21.5 / 19.0, 512 22.4 / 23.0.
+constexpr int64_t kHeldWaves = 2048;
 constexpr int kSumThreads = 1024, kSumWaves = kSumThreads / kWave;
 
 struct RowArgs {
@@ -196,12 +196,70 @@ struct GradArgs {
   const float* logprob;                        // the policy loss
 };
 
-// A workgroup writes kGradSpan vectors of one row's gradient.
+// The sums of the objective over all rows, in double and in a fixed order: one workgroup of W threads, thread i takes rows i, i + W, ...,
+// `kRows` of them on their way at once.
+struct PolicySums {
+  const float *logprob, *entropy;
+  espo_policy_result* out;
+};
+template <int W, int kRows>
+__device__ __forceinline__ void policy_sums(const RowArgs& a, const PolicySums& p, const PolicyArgs& q) {
+  constexpr int kSums = 5, kWaves = W / kWave;
+  __shared__ double lds[kSums + 1][kWaves];
+  double v[kSums + 1] = {};
+#pragma unroll 1
+  for (int64_t first = threadIdx.x; first < a.N; first += kRows * W) {
+    TokenInputs in[kRows];
+    float logprob[kRows], entropy[kRows];
+    int32_t token[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      const int64_t row = first + j * W < a.N ? first + j * W : first;
+      token[j] = first + j * W < a.N ? a.tokens[row] : -1;
+      in[j] = token_inputs(q, row);
+      logprob[j] = p.logprob[row], entropy[j] = p.entropy[row];
+    }
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      if (!used_row(token[j], a.V)) continue;
+      const Surrogate c = surrogate(q, in[j], logprob[j]);
+      const double w = in[j].weight, adv = in[j].adv, H = entropy[j], bound = c.cut ? (adv >= 0.0 ? 1.0 + q.clip_high : 1.0 - q.clip_low) : (double)c.ratio;
+      v[0] += w * (-bound * adv - q.entropy_coef * H);
+      v[1] += w * (-bound * adv);
+      v[2] += w * H;
+      v[3] += w * (exp((double)fminf(c.diff, 88.0f)) - 1.0 - c.diff);
+      v[4] += c.cut ? w : 0.0;
+      v[5] += 1.0;
+    }
+  }
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i <= kSums; ++i) {
+    v[i] = wave_sum_f64(v[i]);
+    if (lane == 0) lds[i][wave] = v[i];
+  }
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int i = 0; i <= kSums; ++i) v[i] = wave_sum_f64(lane < kWaves ? lds[i][lane] : 0.0);
+  if (lane == 0)
+    *p.out = espo_policy_result{(float)v[0], (float)v[1], (float)v[2], (float)v[3], (float)v[4], 0, (int64_t)v[5]};
+}
+
+// A workgroup writes kGradSpan vectors of one row's gradient.  kPolicy: the launch's first workgroup has the objective's sums instead, which a launch
+// of their own would add 3 us for.
 template <int DT, bool kPolicy>
-__global__ __launch_bounds__(kGradThreads) void espo_logits_grad_kernel(RowArgs a, GradArgs d, PolicyArgs q) {
+__global__ __launch_bounds__(kGradThreads) void espo_logits_grad_kernel(RowArgs a, GradArgs d, PolicyArgs q, PolicySums p) {
   constexpr int E = vec_elems<DT>();
-  const int64_t row = blockIdx.x / d.spans;
-  const uint32_t base = (uint32_t)(blockIdx.x - row * d.spans) * kGradSpan, nvec = (a.V + E - 1) / E;
+  if constexpr (kPolicy) {
+    if (blockIdx.x == 0) {
+      policy_sums<kGradThreads, 1>(a, p, q);
+      return;
+    }
+  }
+  const uint32_t group = blockIdx.x - (kPolicy ? 1 : 0);
+  const int64_t row = group / d.spans;
+  const uint32_t base = (uint32_t)(group - row * d.spans) * kGradSpan, nvec = (a.V + E - 1) / E;
   const int32_t token = a.tokens[row];
   char* out = d.dlogits + row * d.grad_bytes;
   if (!used_row(token, a.V)) {
@@ -408,36 +466,8 @@ __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))
   }
 }
 
-// The sums of the objective over all rows, in double and in a fixed order: one workgroup, thread i takes rows i, i + 1024, ...
-__global__ __launch_bounds__(kSumThreads) void espo_policy_sums_kernel(const int32_t* tokens, const float* logprob, const float* entropy,
-                                                                       int64_t N, uint32_t V, PolicyArgs q, espo_policy_result* out) {
-  constexpr int kSums = 5;
-  __shared__ double lds[kSums + 1][kSumWaves];
-  double v[kSums + 1] = {};
-  for (int64_t row = threadIdx.x; row < N; row += kSumThreads) {
-    if (!used_row(tokens[row], V)) continue;
-    const TokenInputs in = token_inputs(q, row);
-    const Surrogate c = surrogate(q, in, logprob[row]);
-    const double w = in.weight, H = entropy[row], bound = c.cut ? (in.adv >= 0.0f ? 1.0 + q.clip_high : 1.0 - q.clip_low) : (double)c.ratio;
-    v[0] += w * (-bound * in.adv - q.entropy_coef * H);
-    v[1] += w * (-bound * in.adv);
-    v[2] += w * H;
-    v[3] += w * (exp((double)fminf(c.diff, 88.0f)) - 1.0 - c.diff);
-    v[4] += c.cut ? w : 0.0;
-    v[5] += 1.0;
-  }
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 0; i <= kSums; ++i) {
-    v[i] = wave_sum_f64(v[i]);
-    if (lane == 0) lds[i][wave] = v[i];
-  }
-  __syncthreads();
-  if (wave != 0) return;
-#pragma unroll
-  for (int i = 0; i <= kSums; ++i) v[i] = wave_sum_f64(lane < kSumWaves ? lds[i][lane] : 0.0);
-  if (lane == 0)
-    *out = espo_policy_result{(float)v[0], (float)v[1], (float)v[2], (float)v[3], (float)v[4], 0, (int64_t)v[5]};
+__global__ __launch_bounds__(kSumThreads) void espo_policy_sums_kernel(RowArgs a, PolicySums p, PolicyArgs q) {
+  policy_sums<kSumThreads, 4>(a, p, q);
 }
 
 RowArgs row_args(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens) {
@@ -476,8 +506,8 @@ void forward(const RowArgs& a, const RowOutputs& o, SoftmaxSums* split, hipStrea
 }
 
 template <int DT, bool kPolicy>
-void backward(const RowArgs& a, const GradArgs& d, const PolicyArgs& q, hipStream_t stream) {
-  hipLaunchKernelGGL((espo_logits_grad_kernel<DT, kPolicy>), dim3((unsigned)(a.N * d.spans)), dim3(kGradThreads), 0, stream, a, d, q);
+void backward(const RowArgs& a, const GradArgs& d, const PolicyArgs& q, const PolicySums& p, hipStream_t stream) {
+  hipLaunchKernelGGL((espo_logits_grad_kernel<DT, kPolicy>), dim3((unsigned)(a.N * d.spans) + (kPolicy ? 1 : 0)), dim3(kGradThreads), 0, stream, a, d, q, p);
 }
 
 // Waves of the workgroup that holds a row of V logits, 0 if none does.
@@ -517,17 +547,19 @@ void policy_held(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const
   }
 }
 
-// Log-probabilities, entropy and, if it is wanted, the gradient of the objective.
+// Log-probabilities, entropy, the objective and, if it is wanted, its gradient.
 template <int DT>
-void policy(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, SoftmaxSums* split, hipStream_t stream) {
+void policy(const RowArgs& a, const RowOutputs& o, const GradArgs& d, const PolicyArgs& q, const PolicySums& p, SoftmaxSums* split, hipStream_t stream) {
   const int waves = d.dlogits ? held_waves<DT>(a.V) : 0;
   switch (a.N * waves >= kHeldWaves ? waves : 0) {
-    case 4: return policy_held<DT, 4>(a, o, d, q, stream);
-    case 8: return policy_held<DT, 8>(a, o, d, q, stream);
-    case 16: return policy_held<DT, 16>(a, o, d, q, stream);
+    case 4: policy_held<DT, 4>(a, o, d, q, stream); break;
+    case 8: policy_held<DT, 8>(a, o, d, q, stream); break;
+    case 16: policy_held<DT, 16>(a, o, d, q, stream); break;
+    default:
+      if (a.N > 0) forward<DT>(a, o, split, stream);
+      if (a.N > 0 && d.dlogits) return backward<DT, true>(a, d, q, p, stream);
   }
-  forward<DT>(a, o, split, stream);
-  if (d.dlogits) backward<DT, true>(a, d, q, stream);
+  hipLaunchKernelGGL(espo_policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, stream, a, p, q);
 }
 
 uint32_t grad_spans(int dt, int64_t V) {
@@ -539,8 +571,8 @@ int launched() { return hipGetLastError() == hipSuccess ? ESPO_OK : ESPO_EHIP; }
 
 }  // namespace
 
-// (A launch has fewer than 2^32 threads.)
-bool grad_indexable(int dt, int64_t N, int64_t V) { return N * (int64_t)grad_spans(dt, V) < ((int64_t)1 << 32) / kGradThreads; }
+// (A launch has fewer than 2^32 threads; one workgroup more than the gradient needs is the policy loss's.)
+bool grad_indexable(int dt, int64_t N, int64_t V) { return N * (int64_t)grad_spans(dt, V) + 1 < ((int64_t)1 << 32) / kGradThreads; }
 
 int launch_logprobs(const void* logits, int dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens,
                     float* logprob, float* entropy, float* stats, void* workspace, hipStream_t stream) {
@@ -561,8 +593,8 @@ int launch_logprobs_backward(const void* logits, int dt, int64_t N, int64_t V, i
                              int64_t grad_stride, hipStream_t stream) {
   const RowArgs a = row_args(logits, dt, N, V, row_stride, temperature, tokens);
   const GradArgs d{(char*)dlogits, grad_stride * (dt == ESPO_BF16 ? 2 : 4), grad_spans(dt, V), (const float2*)stats, entropy, dlogprob, dentropy, nullptr};
-  if (dt == ESPO_BF16) backward<ESPO_BF16, false>(a, d, PolicyArgs{}, stream);
-  else backward<ESPO_F32, false>(a, d, PolicyArgs{}, stream);
+  if (dt == ESPO_BF16) backward<ESPO_BF16, false>(a, d, PolicyArgs{}, PolicySums{}, stream);
+  else backward<ESPO_F32, false>(a, d, PolicyArgs{}, PolicySums{}, stream);
   return launched();
 }
 
@@ -579,13 +611,10 @@ int launch_policy_loss(const void* logits, int dt, int64_t N, int64_t V, int64_t
   if (!entropy) entropy = (float*)(stats + N) + N;
   const RowOutputs o{logprob, entropy, stats};
   const GradArgs d{(char*)dlogits, grad_stride * (dt == ESPO_BF16 ? 2 : 4), grad_spans(dt, V), stats, entropy, nullptr, nullptr, logprob};
-  if (N > 0) {
-    SoftmaxSums* split = (SoftmaxSums*)(stats + 2 * N);
-    if (dt == ESPO_BF16) policy<ESPO_BF16>(a, o, d, q, split, stream);
-    else policy<ESPO_F32>(a, o, d, q, split, stream);
-    if (launched() != ESPO_OK) return ESPO_EHIP;
-  }
-  hipLaunchKernelGGL(espo_policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, stream, tokens, logprob, entropy, N, (uint32_t)V, q, out);
+  const PolicySums p{logprob, entropy, out};
+  SoftmaxSums* split = (SoftmaxSums*)(stats + 2 * N);
+  if (dt == ESPO_BF16) policy<ESPO_BF16>(a, o, d, q, p, split, stream);
+  else policy<ESPO_F32>(a, o, d, q, p, split, stream);
   return launched();
 }
 
