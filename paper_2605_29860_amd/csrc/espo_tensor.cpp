@@ -139,7 +139,26 @@ PyObject* address(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"address", (PyCFunction)(void (*)(void))address<false>, METH_FASTCALL, nullptr},
+// gpu_rows(t, V or None, device) -> (address, rows, V, row stride) of a 2-D tensor of logits on that device; None for anything that is not
+// in order, for the caller to say what.
+PyObject* gpu_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 3 || !THPVariable_Check(args[0])) Py_RETURN_NONE;
+  const at::Tensor& t = THPVariable_Unpack(args[0]);
+  if (t.dim() != 2 || !t.is_cuda() || (t.stride(1) != 1 && t.size(1) > 1)) Py_RETURN_NONE;
+  const long long device = PyLong_AsLongLong(args[2]), N = t.size(0), width = t.size(1), V = args[1] == Py_None ? width : PyLong_AsLongLong(args[1]);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  if (t.get_device() != device || V > width) Py_RETURN_NONE;
+  const long long per = 16 / (long long)t.element_size();   // torch may give any stride to a single row
+  return Py_BuildValue("(NLLL)", PyLong_FromVoidPtr(t.data_ptr()), N, V, N <= 1 ? (width + per - 1) / per * per : (long long)t.stride(0));
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {{"gpu_rows", (PyCFunction)(void (*)(void))gpu_rows, METH_FASTCALL, nullptr},
+                         {"address", (PyCFunction)(void (*)(void))address<false>, METH_FASTCALL, nullptr},
                          {"gpu_address", (PyCFunction)(void (*)(void))address<true>, METH_FASTCALL, nullptr},
                          {"entry", (PyCFunction)(void (*)(void))entry, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -360,3 +360,24 @@ def test_few_long_rows_split_with_a_workspace(dtype):
         alone = torch.full((N,), math.nan, device="cuda")
         espo.espo_logprobs(x, 0.8, tokens, alone, workspace=ws)
         check(alone, f["logprob"], R.logprob_bound(f, V), "logprob without the entropy")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_policy_loss_of_few_long_rows(dtype):
+    test_policy_loss(20, 152064, 0.9, 0.01, True, dtype)
+
+
+def test_rows_that_do_not_fit_are_refused():
+    x, tokens, out = torch.zeros(4, 64, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, device="cuda")
+    espo.espo_logprobs(x, 1.0, tokens, out)
+    for bad in (x.t(), x[0], x.cpu(), x[:, ::2]):
+        with pytest.raises(TypeError):
+            espo.espo_logprobs(bad, 1.0, tokens, out)
+    with pytest.raises(espo.EspoError):
+        espo.espo_logprobs(x, 1.0, tokens, out, V=65)
+    with pytest.raises(espo.EspoError):
+        espo.espo_logprobs(x, 1.0, tokens, out, V=-1)
+    with pytest.raises(ValueError):
+        espo.espo_logprobs(torch.zeros(5, 64, device="cuda"), 1.0, tokens, out)
+    espo.espo_logprobs(x[:1, :63], 1.0, tokens, out)            # a single row's stride does not matter
+    assert abs(float(out[0]) + math.log(63)) < 1e-6 and (out[1:] + math.log(64)).abs().max() < 1e-6
