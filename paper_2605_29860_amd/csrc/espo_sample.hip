@@ -13,7 +13,7 @@
 // vectors.  The bins say where the cut is: exactly so for bf16 logits, whose bins hold one value each, and up to one bin's
 // members for fp32 logits, which are then collected and ranked.  Only blocks that reach the cut are read again, or, where those
 // are many, the row.  Rows that the bins do not describe (a largest logit of 128 and more, a cut among logits of -128 and less or a nucleus
-// that they have a share in, a bin with hundreds of members) find their cut by three levels of 2048 bins over the whole key, one pass over the row each.
+// that they have a share in, a bin with thousands of members) find their cut by three levels of 2048 bins over the whole key, one pass over the row each.
 //
 // What follows the stream is a chain of short steps that run once per row, and what they cost is the fetching of their instructions: a first
 // version that unrolled them took 7 us for each of cut, second reading and draw, at any batch size.  So they are loops, of one
@@ -154,7 +154,9 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float of_key(uint32_t key) { return __builtin_bit_cast(float, key >> 31 ? key & 0x7fffffffu : ~key); }
 
 constexpr int kLevelBins = 2048;            // of a level of the search over whole keys: 11, 11 and 10 bits
-constexpr int kMostMembers = 512;           // logits of a bin that are ranked, each against all others
+// Logits of a bin that are ranked, each against all others.  (V = 152064 f32, B = 128, settings of all kinds: 518 us with 512 of them, because a few rows
+// went to whole keys, 159 with these.)
+constexpr int kMostMembers = 2048;
 constexpr int kMostFew = 400;               // top-k up to this ranks the k largest of fp32 logits, with their bin's others
 constexpr uint32_t kMostRounds = 8;         // of the workgroup over the blocks that are visited; beyond that the row is streamed again
 
@@ -1164,29 +1166,31 @@ size_t filter_lds(int64_t V, uint32_t& blocks, uint32_t& members) {
 
 // Workgroups that a row is split over: as many as the idle compute units allow, of enough tiles each.  A draw without filters gains from
 // 32 tiles each on (two per wave), bf16 logits in rows of 256 tiles; a filtered one, whose parts hand their bins on, in
-// rows of 256 tiles and from three parts of 64 tiles on.  us, whole rows / split (T = 1): V = 152064 bf16, plain B = 1 21.5 / 14.7, 64 23.8 / 18.5,
+// rows of 256 tiles and from three parts of 64 tiles on.  Of fp32 logits under top-p, which take longest, three parts pay from 192 tiles on, two from 512.  us, whole rows / split (T = 1): V = 152064 bf16, plain B = 1 21.5 / 14.7, 64 23.8 / 18.5,
 // 128 24.5 / 22.4; nucleus of 0.7 B = 1 25.6 / 21.7, 64 29.5 / 28.1, 128 30.3 / 31.5 in two parts; V = 152064 f32, B = 32: plain 32.8 / 14.2,
-// nucleus 80 / 51; V = 50003 bf16, B = 32, in three parts: plain 14.7 / 16.1, nucleus 18.5 / 21.0; V = 32768 f32, B = 4: plain 11.5 / 10.3, top-k 50
+// nucleus 83 / 44, B = 128 in two parts 89 / 74; V = 50003 f32, B = 16 36.3 / 30.9, 64 37.1 / 35.8, 100 in two parts 38.2 / 39.2; V = 50003 bf16, B = 32, in three parts: plain 14.7 / 16.1, nucleus 18.5 / 21.0; V = 32768 f32, B = 4: plain 11.5 / 10.3, top-k 50
 // in two parts 16.1 / 18.8.
 constexpr int64_t kComputeUnits = 256;
+enum Draws { kPlainDraws, kFilteredDraws, kNucleusDraws };  // without filters, with some, with top-p among them
 template <int DT>
-uint32_t parts_of(int64_t B, int64_t V, bool filters) {
+uint32_t parts_of(int64_t B, int64_t V, Draws draws) {
+  const bool filters = draws != kPlainDraws, masses = DT != ESPO_BF16 && draws == kNucleusDraws;
   const int64_t tiles = V / (kWave * vec_elems<DT>());
-  if (V > (1 << 19) || ((filters || DT == ESPO_BF16) && tiles < 256)) return 1;
+  if (V > (1 << 19) || ((filters || DT == ESPO_BF16) && tiles < (masses ? 192 : 256))) return 1;
   int64_t n = kComputeUnits / B;
   if (n > tiles / (filters ? 64 : 32)) n = tiles / (filters ? 64 : 32);
   if (n > kMostParts) n = kMostParts;
-  return n < (filters ? 3 : 2) ? 1u : (uint32_t)n;
+  return n < (filters && !(masses && tiles >= 512) ? 3 : 2) ? 1u : (uint32_t)n;
 }
 
 template <int DT>
-SplitLayout split_layout(int64_t B, int64_t V, bool filters) {
+SplitLayout split_layout(int64_t B, int64_t V, Draws draws) {
   const size_t tile = kWave * vec_elems<DT>(), ntiles = (V + tile - 1) / tile, chunks = (ntiles + kChunk - 1) / kChunk;
   size_t front = ntiles * (kWave / kBlockVecs) * 4;
   if (front < chunks * 12) front = chunks * 12;
   front = (front + 15) / 16 * 16;
-  const size_t bins = filters ? kCountBytes + (DT == ESPO_BF16 ? 0 : (size_t)(kBins + 1) / 2 * 16) : 0;
-  SplitLayout l{nullptr, 0, bins, parts_of<DT>(B, V, filters), (uint32_t)front};
+  const size_t bins = draws != kPlainDraws ? kCountBytes + (DT == ESPO_BF16 ? 0 : (size_t)(kBins + 1) / 2 * 16) : 0;
+  SplitLayout l{nullptr, 0, bins, parts_of<DT>(B, V, draws), (uint32_t)front};
   l.row = (front + l.parts * (sizeof(PartRecord) + l.bins) + 255) / 256 * 256;
   return l;
 }
@@ -1194,7 +1198,7 @@ SplitLayout split_layout(int64_t B, int64_t V, bool filters) {
 template <int DT, bool kFilters>
 void launch(SampleArgs& a, int64_t B, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   const size_t lds = kFilters ? filter_lds<DT>(a.V, a.lds_blocks, a.lds_members) : plain_lds<DT>(a.V);
-  a.split = split_layout<DT>(B, a.V, kFilters);
+  a.split = split_layout<DT>(B, a.V, a.top_p ? kNucleusDraws : kFilters ? kFilteredDraws : kPlainDraws);
   if (a.split.parts > 1 && workspace && workspace_bytes >= (size_t)B * a.split.row && (uintptr_t)workspace % 16 == 0) {
     a.split.base = (char*)workspace;
     hipLaunchKernelGGL((espo_sample_part_kernel<DT, kFilters>), dim3((unsigned)(B * a.split.parts)), dim3(kPartWaves * kWave), lds, stream, a);
@@ -1218,8 +1222,8 @@ void launch(SampleArgs& a, int64_t B, void* workspace, size_t workspace_bytes, h
 
 size_t sample_workspace(int dt, int64_t B, int64_t V) {
   size_t most = 0;
-  for (bool filters : {false, true}) {
-    const SplitLayout l = dt == ESPO_BF16 ? split_layout<ESPO_BF16>(B, V, filters) : split_layout<ESPO_F32>(B, V, filters);
+  for (Draws draws : {kPlainDraws, kFilteredDraws, kNucleusDraws}) {
+    const SplitLayout l = dt == ESPO_BF16 ? split_layout<ESPO_BF16>(B, V, draws) : split_layout<ESPO_F32>(B, V, draws);
     if (l.parts > 1 && (size_t)B * l.row > most) most = (size_t)B * l.row;
   }
   return most;

@@ -203,6 +203,29 @@ def test_filters_around_128(T, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("members", [400, 600, 1500, 2048, 2049, 6000])
+def test_crowded_bins(members, dtype):
+    """Many logits next to each other, from a run that is ranked to one that is not, above and below the others."""
+    print(f"[case] sample {members} logits within 1 / 32 {dtype}", flush=True)
+    V = 20001
+    for B, level in ((3, 4.0), (260, -4.03125)):
+        x, g = logits(B, V, dtype, seed=members, scale=1.0)
+        at = torch.randperm(V, generator=g)[:members].cuda()
+        x[:, at] = (level + torch.rand(B, members, generator=g) * 0.031).to(dtype).cuda()
+        if B > 3:
+            x[:, at[0]] = 9.0
+        u = torch.rand(B, generator=g)
+        keep = slice(0, 3)
+        for mode in (dict(p=0.6), dict(k=300), dict(k=350, p=0.4), dict(k=V - members // 2), dict(k=V - members // 2, p=0.99), dict(p=0.9999)):
+            s = {name: torch.full((B,), float(v), device="cuda") if name == "p" else torch.full((B,), v, dtype=torch.int32, device="cuda") for name, v in mode.items()}
+            run(x[keep], u[keep], **mode)
+            tokens, few = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (B, 3))
+            espo.espo_sample(x, u.cuda(), tokens, top_k=s.get("k"), top_p=s.get("p"))
+            espo.espo_sample(x[keep], u[keep].cuda(), few, top_k=s["k"][keep] if "k" in s else None, top_p=s["p"][keep] if "p" in s else None)
+            assert torch.equal(tokens[keep], few)              # 8 waves a row in large batches, 16 in small ones
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_longest_rows(dtype):
     print(f"[case] sample longest rows {dtype}", flush=True)
     for V, modes in ((1 << 19, (dict(), dict(k=60, p=0.9), dict(p=0.8), dict(T=3.0, k=30000, min_p=1e-4))), (1 << 20, (dict(), dict(T=0.4), dict(T=0.0)))):
