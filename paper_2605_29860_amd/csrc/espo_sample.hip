@@ -501,7 +501,7 @@ __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, 
   constexpr uint32_t E = vec_elems<ESPO_BF16>();
   double* table = (double*)lds;
   const auto weight = [&](float x) {
-    const double w = r.weight(x);
+    const double w = exp2_f64(fmin(((double)x - r.m) * r.c, 1000.0));  // the table has entries above the largest logit too
     return x >= keep.cut && w >= keep.min_p ? w : 0.0;
   };
   float is = 0.0f;
@@ -929,11 +929,12 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
     double zero = 0.0;
     if constexpr (kOne) {
       block_before<W>(next_to_0, s.wave_f64[1], zero);
-      zero *= exp2_f64(-r.m * r.c);
+      zero = zero > 0.0 ? zero * exp2_f64(-r.m * r.c) : 0.0;
     }
     const auto bin_mass = [&](int bin) {
       double n = kOne ? (double)count[bin] : (double)mass[bin] * (1.0 / kBinMass);
-      n *= r.weight(bin_number(bin));
+      // by a select: above the largest logit, where bins are empty, a weight may be beyond the range of exp2_f64, and no number
+      n = n > 0.0 ? n * r.weight(bin_number(bin)) : 0.0;
       if (kOne && bin == kBinZero) n = zero;
       if (ranked && bin == kbin) n = (double)s.kept_mass * (1.0 / kFixed);
       return bin < kbin ? 0.0 : n;

@@ -1,0 +1,73 @@
+"""espo_sample, espo_logprobs and espo_policy_loss where exponents leave the ordinary range: low temperatures, logits far from 0, masks
+that hide the first tiles, weights of 0 (needs an MI355X).  The definitions are those of tests/rows_reference.py in 64 bits, and tokens have
+to be equal."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import rows_reference as R  # noqa: E402
+import paper_2605_29860_amd as espo  # noqa: E402
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def padded(x, fill=50.0):
+    """x [B, V] of the CPU as a view of rows that start at multiples of 16 bytes, on the GPU; behind V lies `fill`."""
+    E = 8 if x.dtype == BF16 else 4
+    buf = torch.full((x.shape[0], -(-x.shape[1] // E) * E), fill, dtype=x.dtype)
+    buf[:, :x.shape[1]] = x
+    return buf.cuda()[:, :x.shape[1]]
+
+
+def draw(x, u, T=None, k=None, p=None):
+    """Draws from x [B, V] (on the CPU, settings [B]) with and without a workspace, and compares with the definition.  The sums' errors are below
+    1e-9 of the total here, so a u that comes closer than that to a running sum would decide nothing, nor a p that
+    does to the mass above a logit."""
+    B, V = x.shape
+    gpu = padded(x)
+    dev = lambda t: None if t is None else t.cuda()
+    n = espo.espo_sample_workspace_bytes(B, V, x.dtype)
+    ws = torch.full((n,), 0xCD, dtype=torch.uint8, device="cuda") if n else None
+    tokens, again = (torch.full((B,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    lp = torch.full((B,), math.nan, device="cuda")
+    espo.espo_sample(gpu, u.cuda(), tokens, logprob=lp, temperature=dev(T), top_k=dev(k), top_p=dev(p), workspace=ws)
+    espo.espo_sample(gpu, u.cuda(), again, temperature=dev(T), top_k=dev(k), top_p=dev(p))
+    tokens, lp = tokens.cpu(), lp.cpu()
+    at = lambda t, b, off: off if t is None else float(t[b])
+    wrong = []
+    for b in range(B):
+        tok, want, near = R.sample_row(x[b].double(), at(T, b, 1.0), at(k, b, 0), at(p, b, 1.0), 0.0, float(u[b]))
+        assert near > 1e-9, ("this input decides nothing", b, near)
+        if int(tokens[b]) != tok or not abs(float(lp[b]) - want) <= 2.0 ** -24 * abs(want) + 1e-9:
+            wrong.append((b, at(T, b, 1.0), at(p, b, 1.0), int(tokens[b]), tok, float(lp[b]), want))
+    assert not wrong, (len(wrong), wrong[:4])
+    assert torch.equal(tokens, again.cpu())
+
+
+def settings(values, B, g, dtype=F32):
+    return torch.tensor(values, dtype=dtype)[torch.randint(len(values), (B,), generator=g)]
+
+
+def hot_rows(B, V, dtype, g):
+    """Largest logits from 6 to 60, some hundred different ones below them."""
+    x = torch.randn(B, V, generator=g) * 2.0
+    top = torch.linspace(6.0, 60.0, B)[torch.randperm(B, generator=g)]
+    for b in range(B):
+        at = torch.randperm(V, generator=g)[:300]
+        x[b, at] = top[b] * torch.rand(300, generator=g)
+        x[b, at[:20]] = top[b] - 0.4 * torch.rand(20, generator=g)
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,V", [(200, 9001), (300, 9001), (30, 152064)])
+def test_nuclei_at_low_temperatures(B, V, dtype):
+    print(f"[case] low temperature nuclei B={B} V={V} {dtype}", flush=True)
+    g = torch.Generator().manual_seed(B + V)
+    x = hot_rows(B, V, dtype, g)
+    T, p = settings([0.02, 0.05, 0.07, 0.1, 0.12, 0.15], B, g), settings([0.5, 0.7, 0.95], B, g)
+    draw(x, torch.rand(B, generator=g), T=T, p=p)
+    draw(x, torch.rand(B, generator=g), T=T, p=p, k=settings([0, 500, 2000, 30], B, g, torch.int32))
