@@ -515,6 +515,7 @@ __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, 
           const float top = block_max<W>(max_of<E>(y), s);
           r.m = top > kMaskedRow ? (double)top : 0.0;
           if (!(((double)kBinsBelow - r.m) * r.c < 1000.0)) {  // weights would not be numbers
+            __syncthreads();                // the caller's block_max writes what this one has left
             is = 2.0f;
             return false;
           }

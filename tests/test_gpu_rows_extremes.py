@@ -71,3 +71,15 @@ def test_nuclei_at_low_temperatures(B, V, dtype):
     T, p = settings([0.02, 0.05, 0.07, 0.1, 0.12, 0.15], B, g), settings([0.5, 0.7, 0.95], B, g)
     draw(x, torch.rand(B, generator=g), T=T, p=p)
     draw(x, torch.rand(B, generator=g), T=T, p=p, k=settings([0, 500, 2000, 30], B, g, torch.int32))
+
+
+@pytest.mark.parametrize("B,V", [(5, 9001), (300, 9001), (3, 152064)])
+@pytest.mark.parametrize("top", [-10.0, 0.0, 1.5, 12.0])
+def test_unfiltered_bf16_rows_around_the_lowest_temperature_of_the_table(top, B, V):
+    """Where (128 - the largest logit) log2 e / T crosses 1000 the weights are not taken from a table any more."""
+    print(f"[case] table's lowest temperature, top {top}, B={B} V={V}", flush=True)
+    g = torch.Generator().manual_seed(B + V)
+    x = top - 3.0 * torch.rand(B, V, generator=g)
+    edge = (128.0 - top) * math.log2(math.e) / 1000.0
+    T = edge * settings([0.5, 0.9, 0.97, 0.99, 1.0, 1.01, 1.03, 1.2], B, g)
+    draw(x.to(BF16), torch.rand(B, generator=g), T=T)
