@@ -83,3 +83,17 @@ def test_unfiltered_bf16_rows_around_the_lowest_temperature_of_the_table(top, B,
     edge = (128.0 - top) * math.log2(math.e) / 1000.0
     T = edge * settings([0.5, 0.9, 0.97, 0.99, 1.0, 1.01, 1.03, 1.2], B, g)
     draw(x.to(BF16), torch.rand(B, generator=g), T=T)
+
+
+@pytest.mark.parametrize("T", [1e-3, 3e-4, 1e-4, 5e-5, 1e-5])
+def test_fp32_nuclei_next_to_0(T):
+    """Logits on both sides of 2^-10, the end of the bin of 0, at temperatures that tell them apart."""
+    print(f"[case] nuclei next to 0, T={T}", flush=True)
+    g = torch.Generator().manual_seed(int(1 / T))
+    B, V = 40, 5001
+    x = torch.full((B, V), -1.0)
+    at = torch.randperm(V, generator=g)[:600]
+    x[:, at] = (torch.rand(B, 600, generator=g) * 2.4 - 1.2) * 2.0 ** -10
+    p = settings([0.3, 0.5, 0.7, 0.95], B, g)
+    draw(x, torch.rand(B, generator=g), T=torch.full((B,), T), p=p)
+    draw(x, torch.rand(B, generator=g), T=torch.full((B,), T), p=p, k=torch.full((B,), 550, dtype=torch.int32))
