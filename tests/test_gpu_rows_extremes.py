@@ -97,3 +97,21 @@ def test_fp32_nuclei_next_to_0(T):
     p = settings([0.3, 0.5, 0.7, 0.95], B, g)
     draw(x, torch.rand(B, generator=g), T=torch.full((B,), T), p=p)
     draw(x, torch.rand(B, generator=g), T=torch.full((B,), T), p=p, k=torch.full((B,), 550, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("T", [0.1, 0.02, 0.01, 1e-3, 1e-5])
+def test_fp32_nuclei_of_negative_logits(T):
+    """Rows with nothing above 0, as of log-probabilities, whose largest logit is up to 10^7 temperatures below it."""
+    print(f"[case] nuclei of negative logits, T={T}", flush=True)
+    g = torch.Generator().manual_seed(int(1 / T))
+    B, V = 40, 5001
+    top = -torch.logspace(-1, 2.09, B)
+    x = top[:, None] * (1.5 + torch.rand(B, V, generator=g))
+    for b in range(B):
+        at = torch.randperm(V, generator=g)[:500]
+        x[b, at] = top[b] - 6 * T * torch.rand(500, generator=g)
+    x[0, :2], x[1, :2] = torch.tensor([-100.49, -100.5]), torch.tensor([-7.99, -8.0])
+    x[:2, 2:] = -130.0
+    p = settings([0.3, 0.5, 0.7, 0.95], B, g)
+    draw(x, torch.rand(B, generator=g), T=torch.full((B,), T), p=p)
+    draw(x, torch.rand(B, generator=g), T=torch.full((B,), T), p=p, k=torch.full((B,), 450, dtype=torch.int32))
