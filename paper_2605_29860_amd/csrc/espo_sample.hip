@@ -495,7 +495,8 @@ __device__ __forceinline__ void stream_chunks(const RowView& r, uint32_t c0, uin
 // less than half the time of a power of 2 in double (B = 512, V = 152064, plain: 62 -> 41 us).  Logits next to 0, of which one bin
 // holds many, are weighed one by one; those of -128 and less count as nothing, and the caller sees to it that they may.  Weights are relative to
 // r.m, the row's largest logit, or if that is not known (`find`) to the largest one of the waves' first tiles, which r.m then becomes: any
-// logit near the top does.  Returns the largest of what the thread's sums are: 0 nothing, 1 numbers, 2 no use (a logit of 128 or more).
+// logit near the top does.  Returns the largest of what the thread's sums are: 0 nothing, 1 numbers, 2 no use (a logit of 128 or
+// more, a low temperature, or first tiles that are masked throughout).
 template <int W>
 __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, const Kept& keep, bool find, unsigned char* lds, double* sums, SampleShared<W>& s) {
   constexpr uint32_t E = vec_elems<ESPO_BF16>();
@@ -513,8 +514,9 @@ __device__ __forceinline__ float sum_by_table(Row& r, uint32_t c0, uint32_t c1, 
           float y[E];
           tile_logits<ESPO_BF16>(r, t, raw, y);
           const float top = block_max<W>(max_of<E>(y), s);
-          r.m = top > kMaskedRow ? (double)top : 0.0;
-          if (!(((double)kBinsBelow - r.m) * r.c < 1000.0)) {  // weights would not be numbers
+          r.m = (double)top;
+          // Weights would not be numbers; or all is masked, and nothing is known of the largest logit that those of -128 and less have to be far below.
+          if (!(((double)kBinsBelow - r.m) * r.c < 1000.0) || !(top > kMaskedRow)) {
             __syncthreads();                // the caller's block_max writes what this one has left
             is = 2.0f;
             return false;

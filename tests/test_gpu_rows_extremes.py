@@ -115,3 +115,17 @@ def test_fp32_nuclei_of_negative_logits(T):
     p = settings([0.3, 0.5, 0.7, 0.95], B, g)
     draw(x, torch.rand(B, generator=g), T=torch.full((B,), T), p=p)
     draw(x, torch.rand(B, generator=g), T=torch.full((B,), T), p=p, k=torch.full((B,), 450, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,V", [(6, 9001), (300, 9001), (4, 152064)])
+def test_masks_that_leave_low_logits_outside_the_first_tiles(B, V, dtype):
+    """Nothing is left in the first quarter of every 2048 logits, and what is left lies on both sides of -128."""
+    print(f"[case] low logits outside the first tiles B={B} V={V} {dtype}", flush=True)
+    g = torch.Generator().manual_seed(B + V)
+    x = torch.full((B, V), -math.inf)
+    for b in range(B):
+        at = 2048 * torch.randint(V // 2048, (8,), generator=g) + 600 + torch.randint(1400, (8,), generator=g)
+        x[b, at] = -120.0 - 24.0 * torch.rand(8, generator=g)
+    T = settings([1.0, 2.0, 5.0, 20.0], B, g)
+    draw(x.to(dtype), torch.rand(B, generator=g), T=T)
