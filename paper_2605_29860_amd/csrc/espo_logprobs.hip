@@ -42,14 +42,13 @@ struct RowOutputs {  // of a forward pass; what is not wanted is null
 
 __device__ __forceinline__ bool used_row(int32_t token, uint32_t V) { return (uint32_t)token < V; }  // a negative token is beyond any V
 
-// What a row's sums come to.  A row without any logit has the statistics of an empty sum, and its token is masked.
-__device__ __forceinline__ void row_results(const RowArgs& a, float x_token, const SoftmaxSums& p, float& logprob, float& entropy, float2& stats) {
-  const bool any = p.m > kMaskedRow;
-  const SoftmaxSums q = exact_sums(p, a.k2);
+// What a row's sums (of row_sums) come to.  A row without any logit has the statistics of an empty sum, and its token is masked.
+__device__ __forceinline__ void row_results(const RowArgs& a, float x_token, const SoftmaxSums& q, float& logprob, float& entropy, float2& stats) {
+  const bool any = q.m > kMaskedRow;
   const float ln_s = any ? logf(q.s) : 0.0f;
-  logprob = x_token > kMaskedRow ? -(p.m - x_token) * a.inv_t - ln_s : kNegInf;
+  logprob = x_token > kMaskedRow ? -(q.m - x_token) * a.inv_t - ln_s : kNegInf;
   entropy = any ? ln_s - q.a * __builtin_amdgcn_rcpf(q.s) * kLn2 : 0.0f;
-  stats = any ? float2{p.m, q.s} : float2{0.0f, 1.0f};
+  stats = any ? float2{q.m, q.s} : float2{0.0f, 1.0f};
 }
 
 __device__ __forceinline__ void store_row(const RowOutputs& o, int64_t row, float logprob, float entropy, float2 stats) {
@@ -107,7 +106,7 @@ __global__ __launch_bounds__(kRowThreads) void espo_logprobs_kernel(RowArgs a, R
     const SoftmaxSums p = sum_tiles<DT, kEntropy>(a, r, t0, min(t0 + each, r.ntiles), lds);
     if (threadIdx.x == 0) split[blockIdx.x] = p;
   } else {
-    const SoftmaxSums p = sum_tiles<DT, kEntropy>(a, r, 0, r.ntiles, lds);
+    const SoftmaxSums p = row_sums<DT, kRowWaves>(r, sum_tiles<DT, kEntropy>(a, r, 0, r.ntiles, lds), a.k2, lds);
     if (threadIdx.x == 0) {
       float logprob, entropy;
       float2 stats;
@@ -125,8 +124,9 @@ __global__ __launch_bounds__(kWave) void espo_logprobs_join_kernel(RowArgs a, Ro
   float logprob = 0.0f, entropy = 0.0f;
   float2 stats{0.0f, 1.0f};
   if (used_row(token, a.V)) {
+    const char* x = a.logits + row * a.row_bytes;
     const SoftmaxSums p = wave_merge<kEntropy>(threadIdx.x < parts ? split[row * parts + threadIdx.x] : kNoSums, a.k2);
-    row_results(a, logit_at<DT>(a.logits + row * a.row_bytes, (uint32_t)token), p, logprob, entropy, stats);
+    row_results(a, logit_at<DT>(x, (uint32_t)token), row_sums<DT, 1>(row_view<DT>(x, a.V), p, a.k2, nullptr), logprob, entropy, stats);
   }
   if (threadIdx.x == 0) store_row(o, row, logprob, entropy, stats);
 }
@@ -160,15 +160,22 @@ __device__ __forceinline__ Surrogate surrogate(const PolicyArgs& q, const TokenI
 
 // A row's gradient: dx_v = 2^t (p0 + p1 t) with t = x_v k2 + nb, and `at` more at the token.
 struct RowGrad {
-  float nb, p0, p1, at;
+  float k2, nb, p0, p1, at;
 };
+
+// k2 for a row's gradient.  From kFarLane on nb's rounding alone would be no number as a power of 2, and nothing but the largest logit has a
+// weight: then any factor does that keeps logits which differ apart, and m times a power of 2 is exact.
+__device__ __forceinline__ float grad_slope(float m, float k2) {
+  if (fabsf(m * k2) < kFarLane) return k2;
+  return __builtin_bit_cast(float, (286u << 23) - (__builtin_bit_cast(uint32_t, m) & 0x7f800000u));  // |m| times this is 2^32 to 2^33, neighbours differ by 2^9
+}
 
 // m, s: the row's largest logit and sum; `entropy` only counts where h is not 0.
 __device__ __forceinline__ RowGrad row_grad(const RowArgs& a, float m, float s, float entropy, float g, float h) {
 #pragma clang fp contract(off)  // nb is a rounded product
-  const float nb = -m * a.k2, d = exponent_short(m, nb, a.k2);  // t is short by the rounding of nb, and 2^t by a factor
+  const float k2 = uniform_f32(grad_slope(m, a.k2), 0), nb = -m * k2, d = exponent_short(m, nb, k2);  // t is short by the rounding of nb, and 2^t by a factor
   const float per = a.inv_t * __builtin_amdgcn_rcpf(s) * __builtin_amdgcn_exp2f(d), p1 = -h * kLn2 * per;
-  return RowGrad{nb, p1 * d - (h != 0.0f ? g + h * (entropy - logf(s)) : g) * per, p1, g * a.inv_t};
+  return RowGrad{k2, nb, p1 * d - (h != 0.0f ? g + h * (entropy - logf(s)) : g) * per, p1, g * a.inv_t};
 }
 
 template <int DT, bool kSlope>
@@ -180,7 +187,7 @@ __device__ __forceinline__ u32x4 grad_vec(const RowArgs& a, const RowGrad& c, u3
 #pragma unroll
   for (int k = 0; k < E; ++k) {
     const float x = y[k];
-    float t = __builtin_fmaf(x, a.k2, c.nb);
+    float t = __builtin_fmaf(x, c.k2, c.nb);
     if constexpr (kSlope) t = fmaxf(t, kLeastExponent);
     const float e = __builtin_amdgcn_exp2f(t);
     y[k] = e * (kSlope ? __builtin_fmaf(c.p1, t, c.p0) : c.p0);
@@ -438,7 +445,7 @@ __global__ __launch_bounds__(W* kWave) __attribute__((amdgpu_waves_per_eu(4, 4))
 #pragma unroll
       for (uint32_t k = 0; k < E; ++k) add_logit<true>(p, y[k], a.k2);
     }
-    p = block_merge<W, true>(p, a.k2, lds[i & 1]);
+    p = row_sums<DT, W>(row_view<DT>(a.logits + row * a.row_bytes, a.V), block_merge<W, true>(p, a.k2, lds[i & 1]), a.k2, lds[i & 1]);
     float logprob, entropy;
     float2 stats;
     row_results(a, token_logit[i & 1], p, logprob, entropy, stats);

@@ -173,9 +173,13 @@ __device__ __forceinline__ float logit_at(const char* row, uint32_t v) {
 }
 
 // Softmax sums of the logits seen so far: s = sum 2^t, a = sum t 2^t with t = x k2 + nb, k2 = log2(e) / temperature and nb = -m k2
-// rounded, m the largest logit.  One fused operation forms t, with an error of 2^-24 |t| however large m k2 is; that nb is rounded
-// scales both sums by one factor, which exact_sums takes out.  m starts at kMaskedRow, and sums over nothing but masked
+// rounded, m the largest logit.  One fused operation forms t with one rounding; that nb is rounded moves every t by the same d of up to half a
+// step of nb, which scales both sums by one factor, and row_sums takes it out.  m starts at kMaskedRow, and sums over nothing but masked
 // logits are dropped.
+// Where |nb| is large, so is d.  From kFarRow on (below it d is at most 8) a row's sums are formed again from the differences x - m.  From kFarLane on
+// 2^d may be no number (below it d is at most 64), but two logits that differ are 128 powers of 2 and more apart, so that what a lane has summed up relative to
+// one that is not the row's largest counts as nothing.
+constexpr float kFarRow = 0x1p28f, kFarLane = 0x1p31f;
 struct SoftmaxSums {
   float m, nb, s, a;
 };
@@ -184,7 +188,7 @@ constexpr SoftmaxSums kNoSums = SoftmaxSums{kMaskedRow, 0.0f, 0.0f, 0.0f};
 template <bool kEntropy>
 __device__ __forceinline__ void rescale(SoftmaxSums& p, float m, float k2) {
 #pragma clang fp contract(off)  // the difference of two references is that of their rounded values
-  const bool any = p.m > kMaskedRow;
+  const bool any = p.m > kMaskedRow && fabsf(p.nb) < kFarLane;
   const float nb = -m * k2, d = fmaxf(nb - p.nb, kLeastExponent), f = any ? __builtin_amdgcn_exp2f(d) : 0.0f, s = any ? p.s : 0.0f;
   if constexpr (kEntropy) p.a = f * ((any ? p.a : 0.0f) + d * s);
   p.s = s * f;
@@ -229,12 +233,45 @@ __device__ __forceinline__ SoftmaxSums block_merge(SoftmaxSums p, float k2, Soft
 // By how much t falls short of (x - m) k2.
 __device__ __forceinline__ float exponent_short(float m, float nb, float k2) { return __builtin_fmaf(-m, k2, -nb); }
 
-// The sums relative to m itself.  The largest logit's own term is 1, and 0 in a, by definition: it is taken out as it was added and put
-// back as that, so that a row of one logit has the sums 1 and 0.
+// The sums relative to m itself, of a row with |nb| below kFarRow.  The largest logit's own term is 1, and 0 in a, by definition: it is taken out
+// as it was added and put back as that, so that a row of one logit has the sums 1 and 0.
 __device__ __forceinline__ SoftmaxSums exact_sums(const SoftmaxSums& p, float k2) {
   const float d = exponent_short(p.m, p.nb, k2), f = __builtin_amdgcn_exp2f(d), t = __builtin_fmaf(p.m, k2, p.nb), e = __builtin_amdgcn_exp2f(t);
   const float s = p.s - e, a = p.a - e * t;
   return SoftmaxSums{p.m, p.nb, __builtin_fmaf(s, f, 1.0f), f * __builtin_fmaf(d, s, a)};
+}
+
+// The same of a row with |nb| of kFarRow and more, from the row itself, by a workgroup of W waves.
+template <int DT, int W>
+__device__ __forceinline__ SoftmaxSums far_sums(const RowView& r, float m, float k2, SoftmaxSums* lds) {
+  float s = 0.0f, a = 0.0f;
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x; i < r.nvec; i += W * kWave) {
+    const u32x4 raw = vec_load<DT>(r.x, i, r.V);
+#pragma unroll 1
+    for (uint32_t j = 0; j < vec_elems<DT>(); ++j) {
+      const float x = logit_in<DT>(raw, j), t = fmaxf((x - m) * k2, kLeastExponent), e = x > kMaskedRow ? __builtin_amdgcn_exp2f(t) : 0.0f;
+      s += e;
+      a = __builtin_fmaf(e, t, a);
+    }
+  }
+  s = wave_sum(s), a = wave_sum(a);
+  if constexpr (W > 1) {
+    const int lane = threadIdx.x & (kWave - 1);
+    __syncthreads();                          // block_merge's sums have been read
+    if (lane == 0) lds[threadIdx.x >> 6] = SoftmaxSums{m, 0.0f, s, a};
+    __syncthreads();
+    s = wave_sum(lane < W ? lds[lane].s : 0.0f), a = wave_sum(lane < W ? lds[lane].a : 0.0f);
+  }
+  return SoftmaxSums{m, -m * k2, s, a};
+}
+
+// A row's sums relative to its largest logit, from what was merged over its workgroup of W waves (the same in all threads); lds: block_merge's.
+template <int DT, int W>
+__device__ __forceinline__ SoftmaxSums row_sums(const RowView& r, const SoftmaxSums& p, float k2, SoftmaxSums* lds) {
+  const float m = uniform_f32(p.m, 0), nb = uniform_f32(p.nb, 0);
+  if (m > kMaskedRow && !(fabsf(nb) < kFarRow)) return far_sums<DT, W>(r, m, k2, lds);
+  return exact_sums(p, k2);
 }
 
 }  // namespace espo

@@ -129,3 +129,100 @@ def test_masks_that_leave_low_logits_outside_the_first_tiles(B, V, dtype):
         x[b, at] = -120.0 - 24.0 * torch.rand(8, generator=g)
     T = settings([1.0, 2.0, 5.0, 20.0], B, g)
     draw(x.to(dtype), torch.rand(B, generator=g), T=T)
+
+
+def far_rows(V, dtype, g):
+    """Rows whose largest logit is many temperatures away from 0, on either side, and rows with masks that are not masked for the kernels, each
+    with the temperature to use: [(T, rows)]."""
+    noise = lambda n, scale=1.0: scale * torch.randn(n, V, generator=g)
+    rows = []
+    for T, m in ((1e-6, 9999.0), (1e-6, -300.0), (1e-4, 777777.0), (1e-4, -777777.0), (1.0, -1e10), (1.0, 1e10), (1.0, -3e9), (0.7, 1.5e9), (2.0, 3e38), (1e-6, -1e29)):
+        x = m + noise(3)
+        x[1, V // 3:] = m - abs(m) * 1e-3                       # most of the row clearly lower
+        x[2] = m                                                # all the same
+        rows.append((T, x))
+    for fill in (-1e9, -1e10, -2.5e10, -1e15, -1e20, -9.9e29):
+        x = noise(3, 3.0)
+        x[0, : V // 2] = fill                                   # long runs: lanes that see nothing else for a while or at all
+        x[1, V // 4:] = fill
+        x[2, torch.rand(V, generator=g) < 0.97] = fill
+        rows.append((1.0, x))
+    return [(T, x.to(dtype)) for T, x in rows]
+
+
+def check(got, want, bound, what):
+    got = got.double().cpu()
+    bad = ~((got == want) | ((got - want).abs() <= bound))      # (equal infinities)
+    assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[0].tolist(), float(got[bad][0]), float(want[bad][0]))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V", [5, 3001, 140001])
+def test_logits_many_temperatures_from_0(V, dtype):
+    g = torch.Generator().manual_seed(V)
+    half = torch.finfo(dtype).eps / 2
+    for i, (T, x) in enumerate(far_rows(V, dtype, g)):
+        print(f"[case] far logits {i} T={T} V={V} {dtype}", flush=True)
+        N = 3
+        tokens = torch.tensor([V - 1, 0, V // 2], dtype=torch.int32)
+        gpu = padded(x)
+        f = R.softmax_rows(x.double(), T, tokens)
+        n = espo.espo_logprobs_workspace_bytes(N, V, dtype)
+        for ws in ([None, torch.full((n,), 0xCD, dtype=torch.uint8, device="cuda")] if n else [None]):
+            lp, H, stats = (torch.full((m,), math.nan, device="cuda") for m in (N, N, 2 * N))
+            espo.espo_logprobs(gpu, T, tokens.cuda(), lp, entropy=H, stats=stats, workspace=ws)
+            want = f["logprob"]
+            want = torch.where(want < -torch.finfo(F32).max, -math.inf, want)
+            check(lp, want, R.logprob_bound(f, V), "logprob")
+            check(H, f["entropy"], R.entropy_bound(f, V), "entropy")
+            espo.espo_logprobs(gpu, T, tokens.cuda(), lp, workspace=ws)
+            check(lp, want, R.logprob_bound(f, V), "logprob alone")
+        dlp, dH = torch.randn(N, generator=g), torch.randn(N, generator=g)
+        for h in (None, dH):
+            d = padded(torch.full_like(x, 5.0))
+            espo.espo_logprobs_backward(gpu, T, tokens.cuda(), stats, dlp.cuda(), d, entropy=None if h is None else H,
+                                        dentropy=None if h is None else h.cuda())
+            hh = torch.zeros(N).double() if h is None else h.double()
+            ref = R.logits_grad(f, dlp.double(), hh)
+            check(d, ref, R.grad_bound(f, dlp.double(), hh, ref, half, V), "gradient")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,V,coef,which", [(9, 3001, 0.01, range(16)), (9, 3001, 0.0, range(16)), (1032, 3001, 0.01, range(0, 16, 3)), (1032, 3001, 0.0, range(0, 16, 3)),
+                                            (264, 40001, 0.01, (1, 4, 11))])
+def test_policy_loss_of_logits_many_temperatures_from_0(N, V, coef, which, dtype):
+    """The rows between others, in batches that are read twice and in ones whose rows are held."""
+    g = torch.Generator().manual_seed(N)
+    half = torch.finfo(dtype).eps / 2
+    for i, (T, far) in enumerate(far_rows(V, dtype, g)):
+        if i not in which:
+            continue
+        print(f"[case] policy loss of far logits {i} T={T} N={N} V={V} {dtype}", flush=True)
+        x = (3.0 * T * torch.randn(N, V, generator=g)).to(dtype)
+        at = torch.randperm(N, generator=g)[:3]
+        x[at] = far
+        tokens = x.float().argmax(1).to(torch.int32)
+        f = R.softmax_rows(x.double(), T, tokens)
+        old, adv = f["logprob"].float() - 0.1, torch.randn(N, generator=g)
+        ones = torch.ones(N).double()
+        gg, h, sums, c = R.policy_terms(f, old.double(), adv.double(), ones, 1.0 / N, 0.2, 0.2, coef)
+        out = torch.zeros(espo.POLICY_RESULT_BYTES, dtype=torch.uint8, device="cuda")
+        ws = torch.full((espo.espo_policy_loss_workspace_bytes(N, V, dtype),), 0xCD, dtype=torch.uint8, device="cuda")
+        lp, H = torch.full((N,), math.nan, device="cuda"), torch.full((N,), math.nan, device="cuda")
+        gpu = padded(x)
+        whole = torch.full((N, gpu.stride(0)), 5.0, dtype=dtype, device="cuda")
+        d = whole[:, :V]
+        espo.espo_policy_loss(gpu, T, tokens.cuda(), old.cuda(), adv.cuda(), out, ws, dlogits=d, logprob=lp, entropy=H, entropy_coef=coef,
+                              scale=1.0 / N)
+        check(lp, f["logprob"], R.logprob_bound(f, V), "logprob")
+        check(H, f["entropy"], R.entropy_bound(f, V), "entropy")
+        ref = R.logits_grad(f, gg, h)
+        # the ratio carries the log-probability's error and its own four roundings, relative to g
+        rel = (R.logprob_bound(f, V) + 8 * R.U)[:, None]
+        check(d, ref, R.grad_bound(f, gg, h, ref, half, V) + rel * gg.abs()[:, None] * 2 / T, "gradient")
+        assert (whole[:, V:] == 5.0).all()
+        res = espo.read_policy_result(out)
+        lpb, Hb = R.logprob_bound(f, V) + 8 * R.U, R.entropy_bound(f, V)
+        # weights are a product of two roundings, the sum is rounded to fp32 once
+        err = (c["w"] * (lpb * c["r"] * c["A"].abs() * 2 + coef * Hb)).sum() + 4 * R.U * (c["w"] * (1 + c["r"] * c["A"].abs() + f["entropy"])).sum()
+        assert abs(res["loss"] - float(sums[0])) <= float(err) and res["tokens"] == N
