@@ -581,10 +581,11 @@ size_t espo_logprobs_workspace_bytes(int64_t N, int64_t V, espo_dtype dt);
  *   r < 1 - clip_low); d(loss)/d(entropy[n]) = -w entropy_coef; on the logits as in espo_logprobs_backward.
  * A mean over the valid tokens is scale = 1 / their number (or weights that say otherwise, one per token).  old_logprob is what
  * espo_step or espo_logprobs returned when the tokens were drawn, adv what espo_whiten returned, both in the order of the rows.
- * The exponent of r is held at 88 at most (e^88 is the largest power of e in fp32).
+ * The exponent of r is held at 88 at most (e^88 is the largest power of e in fp32).  A token that is masked has r = 0, and the `kl` of the batch is
+ * then inf, unless the row's weight is 0: such rows add nothing to any sum but `tokens`.
  *
  * Arguments as for espo_logprobs, and
- *   old_logprob, adv   device, [N] fp32; read for used rows only.
+ *   old_logprob, adv   device, [N] fp32; read for used rows only, and finite there.
  *   weights     device, [N] fp32, or NULL for 1.
  *   ctrl        host, read during the call: 0 <= clip_low <= 1, clip_high >= 0, finite entropy_coef and scale.
  *   dlogits, grad_stride   as for espo_logprobs_backward (logits may be overwritten), or NULL for the loss alone.

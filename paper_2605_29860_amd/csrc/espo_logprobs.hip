@@ -236,7 +236,7 @@ __device__ __forceinline__ void policy_sums(const RowArgs& a, const PolicySums& 
       v[0] += w * (-bound * adv - q.entropy_coef * H);
       v[1] += w * (-bound * adv);
       v[2] += w * H;
-      v[3] += w * (exp((double)fminf(c.diff, 88.0f)) - 1.0 - c.diff);
+      v[3] += w != 0.0 ? w * (exp((double)fminf(c.diff, 88.0f)) - 1.0 - c.diff) : 0.0;  // ln r is -inf for a token that is masked
       v[4] += c.cut ? w : 0.0;
       v[5] += 1.0;
     }

@@ -226,3 +226,36 @@ def test_policy_loss_of_logits_many_temperatures_from_0(N, V, coef, which, dtype
         # weights are a product of two roundings, the sum is rounded to fp32 once
         err = (c["w"] * (lpb * c["r"] * c["A"].abs() * 2 + coef * Hb)).sum() + 4 * R.U * (c["w"] * (1 + c["r"] * c["A"].abs() + f["entropy"])).sum()
         assert abs(res["loss"] - float(sums[0])) <= float(err) and res["tokens"] == N
+
+
+@pytest.mark.parametrize("N", [4, 1024])
+def test_weight_0_takes_a_token_out_whose_probability_is_0(N):
+    """A token that the new policy's mask rules out has r = 0 and ln r = -inf; with weight 0 it adds nothing to any sum."""
+    print(f"[case] policy loss, weight 0 and a masked token, N={N}", flush=True)
+    V = 2000
+    g = torch.Generator().manual_seed(N)
+    x = torch.randn(N, V, generator=g)
+    tokens = torch.randint(0, V, (N,), generator=g, dtype=torch.int32)
+    x[1, int(tokens[1])] = -math.inf
+    x[3, int(tokens[3])] = -1e30
+    weights = torch.ones(N)
+    weights[1] = weights[3] = 0.0
+    f = R.softmax_rows(x.double(), 1.0, tokens)
+    old = torch.where(torch.isinf(f["logprob"]), -3.0, f["logprob"]).float() + 0.05
+    adv = torch.randn(N, generator=g)
+    rest = torch.tensor([n for n in range(N) if n not in (1, 3)])
+    part = {k: v[rest] if isinstance(v, torch.Tensor) else v for k, v in f.items()}
+    _, _, sums, c = R.policy_terms(part, old[rest].double(), adv[rest].double(), torch.ones(N - 2).double(), 1.0 / N, 0.2, 0.2, 0.01)
+    out = torch.zeros(espo.POLICY_RESULT_BYTES, dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(espo.espo_policy_loss_workspace_bytes(N, V, F32), dtype=torch.uint8, device="cuda")
+    d = torch.full((N, V), 3.0, device="cuda")
+    espo.espo_policy_loss(x.cuda(), 1.0, tokens.cuda(), old.cuda(), adv.cuda(), out, ws, dlogits=d, weights=weights.cuda(), entropy_coef=0.01,
+                          scale=1.0 / N)
+    res = espo.read_policy_result(out)
+    assert (d[1] == 0).all() and (d[3] == 0).all() and res["tokens"] == N
+    lpb, Hb = R.logprob_bound(part, V) + 8 * R.U, R.entropy_bound(part, V)
+    err = [(c["w"] * (lpb * c["r"] * c["A"].abs() * 2 + 0.01 * Hb)).sum(), (c["w"] * lpb * c["r"] * c["A"].abs() * 2).sum(), (c["w"] * Hb).sum(),
+           (c["w"] * lpb * (1 + c["r"] + c["d"].abs())).sum()]
+    for name, s, e in zip(("loss", "policy", "entropy", "kl"), sums, err):
+        # weights are a product of two roundings; the sums are rounded to fp32 once
+        assert abs(res[name] - float(s)) <= float(e) + 4 * R.U * float((c["w"] * (1 + c["r"] * c["A"].abs() + part["entropy"] + c["d"].abs())).sum()), name
