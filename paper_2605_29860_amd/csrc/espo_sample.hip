@@ -858,11 +858,12 @@ __device__ __forceinline__ void draw_filtered(const SampleArgs& a, int64_t b, Ro
 
   // the cut: logits of at least this are kept, as far as top-k and top-p go
   float cut = -3.402823466e38f;
-  // The bins must hold all logits that have a say, and e^(x / T) of the logits next to 0 must be a number.  A bin's mass must fit: its members
-  // lie within 2^-7 of its number, relative to that, or within 2^-10 of 0, so that near the top none weighs more or less than its number by more than a
-  // factor of e^(300 / 128) = 10.4 (less below 0, where the number is the bin's largest); 2^19 of them in units of 2^-40 stay below 2^63.
-  bool known = (k == 0 && p == 0.0f) ||
-               (top < kBinsBelow && (!masses || fmax(fabs((double)top), 0.125) * r.inv_t < 300.0) && (p == 0.0f || r.inv_t < 300000.0));
+  // The bins must hold all logits that have a say, and e^(x / T) of the logits next to 0 must be a number.  A bin's mass must fit and count: its
+  // members lie within 2^-7 of its number, relative to that, or within 2^-10 of 0.  Above 0 the number is the bin's least: none weighs more than
+  // e^(300 / 128) = 10.4 times what it does, and 2^19 of them in units of 2^-40 stay below 2^63.  Below 0 it is the largest: those
+  // near the top weigh e^(-900 / 128) = 1 / 1130 at least, and half a unit of each is 5e-10 of the mass.
+  const double far = fmax(fmax((double)top, 0.125), -1.0 / 3.0 * (double)top);
+  bool known = (k == 0 && p == 0.0f) || (top < kBinsBelow && (!masses || far * r.inv_t < 300.0) && (p == 0.0f || r.inv_t < 300000.0));
   constexpr int kEach = (kBinHigh + kThreads - 1) / kThreads;  // bins of a thread, from the top
   const int highest = kBinHigh - (int)threadIdx.x * kEach, lowest = max(highest - kEach + 1, kBinLow);
   int kbin = 0;                             // bins below it are out by top-k
