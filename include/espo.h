@@ -498,8 +498,10 @@ int espo_length_order(const int32_t* lengths, int64_t B, int64_t T, int32_t* ord
  *   tokens[b]  = the lowest kept v whose sum of w over the kept indices up to and with v exceeds u[b] W,
  *   logprob[b] = t_a - ln W, the logarithm of the probability it was drawn with.
  * Weights and sums are double, so that the token is the definition's unless u[b] W lies within about 1e-13 W of one of the
- * running sums (weights below 1e-250 count as none).  u[b] in [0, 1); a larger one gives the last kept token, a smaller one the first.  T <= 0 is greedy: the lowest
- * index of the largest logit, logprob 0.  A row whose logits are all masked, and one with alive[b] == 0, whose logits are
+ * running sums (weights below 1e-250 count as none), min_p[b] within 1e-13 of a weight, or top_p[b] within 3e-8 of the share of the mass above
+ * one of the logits (masses that many logits add to are sums of integers).  u[b] in [0, 1); a larger one gives the last kept token, a smaller one the first.  T <= 0 is greedy: the lowest
+ * index of the largest logit, logprob 0.  Temperatures above 1e25 count as 1e25; above 1e20, masked logits take part in rows whose largest logit
+ * is below -1e29.  A row whose logits are all masked, and one with alive[b] == 0, whose logits are
  * not read, has token -1 and logprob 0.  NaN in logits or settings and +inf logits are not supported (results for that
  * row are unspecified, no fault).
  *
@@ -537,7 +539,7 @@ size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
  * the logits' type once, as it is stored.
  * A row whose token is outside [0, V) is not used (padding, a prompt): its logits are not read, logprob and entropy
  * are 0 and its gradient is 0.  Masked logits (at or below -1e30) have probability and gradient 0; a token that is
- * masked itself has logprob -inf.  NaN and +inf are not supported in rows that are used (results for that row are
+ * masked itself has logprob -inf.  (At temperatures above 1e20 this needs a largest logit above -1e29.)  NaN and +inf are not supported in rows that are used (results for that row are
  * unspecified, no fault).
  *
  * Arguments

@@ -16,7 +16,7 @@ SOURCES = [("espo_step.hip", []), ("espo_step.hip", ["-DESPO_STEP_F32"]), ("espo
 # packed-fp32 VALU forms are switched off for every device translation unit
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-               # device code never produces or consumes NaN; this drops the re-quieting of every fmax operand
+               # no result rests on a NaN (a row of logits with one is unspecified); this drops the re-quieting of every fmax operand
                "-Xarch_device", "-fno-honor-nans", "-Xarch_device", "-Wno-nan-infinity-disabled"]
 
 

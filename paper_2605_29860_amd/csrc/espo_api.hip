@@ -119,7 +119,7 @@ int step_checked(const void* logits, espo_dtype dt, int64_t B, int64_t V, int64_
 int rows_checked(const void* logits, espo_dtype dt, int64_t N, int64_t V, int64_t row_stride, float temperature, const int32_t* tokens) {
   if (dt != ESPO_F32 && dt != ESPO_BF16) return ESPO_EINVAL;
   if (N < 0 || V < 1 || row_stride < V) return ESPO_EINVAL;
-  if (!(temperature >= 1e-6f && temperature <= 1e26f)) return ESPO_EINVAL;  // a logit over T stays an fp32 number, and -1e30 over T far from 0
+  if (!(temperature >= 1e-6f && temperature <= 1e26f)) return ESPO_EINVAL;  // -1e30 over T stays an fp32 number, and far from 0
   if (N == 0) return ESPO_OK;
   if (!logits || !tokens) return ESPO_EINVAL;
   if (N >= (1 << 23) || V > (1 << 30)) return ESPO_ERANGE;  // a launch has fewer than 2^32 threads, 512 a row

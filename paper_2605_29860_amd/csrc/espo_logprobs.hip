@@ -22,8 +22,17 @@ constexpr int kGradThreads = 256, kGradLoads = 4;
 constexpr int kGradSpan = kGradThreads * kGradLoads;  // vectors of a workgroup
 constexpr int kComputeUnits = 256, kMostParts = 16;
 // Rows are held by a workgroup each from this many waves on (the chip has 4096 at a time); fewer leave compute units idle, and two passes of
-// smaller workgroups are faster.  us, held / two passes: V = 152064 bf16 (16 waves) N = 64 29.7 / 16.1, 128 31.5 / 30.2, 160 32.2 / 33.2,
-// 256 39.8 / 45.1; V = 70000 bf16 (8 waves) N = 200 22.5 / 21.1, 256 23.7 / 24.5; V = 32000 bf16 (4 waves) N = 400 21.5 / 19.0, 512 22.4 / 23.0.
+// smaller workgroups are faster.  us, held / two passes, by how full the registers of the row's workgroup are:
+//   V = 152064 bf16  16 waves, 98 %  N = 64 31.6 / 18.4   128 32.2 / 30.2   160 32.6 / 33.4   256 40.1 / 43.6   1000 114 / 146
+//   V = 70000 bf16    8 waves, 90 %  N = 200 22.5 / 21.1  256 23.7 / 24.5
+//   V = 32000 bf16    4 waves, 82 %  N = 400 21.5 / 19.0  512 22.4 / 23.0
+//   V = 80000 bf16   16 waves, 51 %  N = 128 23.6 / 17.4  256 26.7 / 26.8   1000 75 / 82
+//   V = 40000 bf16    8 waves, 51 %  N = 256 18.8 / 15.4  512 25.6 / 27.4   4096 140 / 159
+//   V = 20000 bf16    4 waves, 51 %  N = 512 19.1 / 16.2  1024 28.3 / 29.3  4096 85 / 90
+//   V = 8000 bf16     4 waves, 21 %  N = 512 14.7 / 12.0  1024 20.7 / 16.1  4096 58 / 52
+// So the line is near the crossing for full registers (2 us late at 16 waves), for half full ones the crossing is at twice as many rows, and rows
+// of a fifth, whose other loads fetch their last vector again, would always be faster in two passes.  All rows count, used or not: of N = 128
+// with half of them unused, 32.7 / 28.0.
 constexpr int64_t kHeldWaves = 2048;
 constexpr int kSumThreads = 1024, kSumWaves = kSumThreads / kWave;
 

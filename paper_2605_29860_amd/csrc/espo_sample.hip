@@ -13,7 +13,8 @@
 // vectors.  The bins say where the cut is: exactly so for bf16 logits, whose bins hold one value each, and up to one bin's
 // members for fp32 logits, which are then collected and ranked.  Only blocks that reach the cut are read again, or, where those
 // are many, the row.  Rows that the bins do not describe (a largest logit of 128 and more, a cut among logits of -128 and less or a nucleus
-// that they have a share in, a bin with thousands of members) find their cut by three levels of 2048 bins over the whole key, one pass over the row each.
+// that they have a share in, a bin with thousands of members, an fp32 nucleus whose largest logit is beyond 300 T, or 900 T below 0, or whose T is below
+// 4e-4) find their cut by three levels of 2048 bins over the whole key, one pass over the row each.
 //
 // What follows the stream is a chain of short steps that run once per row, and what they cost is the fetching of their instructions: a first
 // version that unrolled them took 7 us for each of cut, second reading and draw, at any batch size.  So they are loops, of one
@@ -1172,10 +1173,18 @@ size_t filter_lds(int64_t V, uint32_t& blocks, uint32_t& members) {
 
 // Workgroups that a row is split over: as many as the idle compute units allow, of enough tiles each.  A draw without filters gains from
 // 32 tiles each on (two per wave), bf16 logits in rows of 256 tiles; a filtered one, whose parts hand their bins on, in
-// rows of 256 tiles and from three parts of 64 tiles on.  Of fp32 logits under top-p, which take longest, three parts pay from 192 tiles on, two from 512.  us, whole rows / split (T = 1): V = 152064 bf16, plain B = 1 21.5 / 14.7, 64 23.8 / 18.5,
-// 128 24.5 / 22.4; nucleus of 0.7 B = 1 25.6 / 21.7, 64 29.5 / 28.1, 128 30.3 / 31.5 in two parts; V = 152064 f32, B = 32: plain 32.8 / 14.2,
-// nucleus 83 / 44, B = 128 in two parts 89 / 74; V = 50003 f32, B = 16 36.3 / 30.9, 64 37.1 / 35.8, 100 in two parts 38.2 / 39.2; V = 50003 bf16, B = 32, in three parts: plain 14.7 / 16.1, nucleus 18.5 / 21.0; V = 32768 f32, B = 4: plain 11.5 / 10.3, top-k 50
-// in two parts 16.1 / 18.8.
+// rows of 256 tiles and from three parts of 64 tiles on.  Of fp32 logits under top-p, which take longest, three parts pay from 192 tiles on, two from 512.
+// us, whole rows / split, at T = 1:
+//   V = 152064 bf16  plain           B = 1 21.5 / 14.7   64 23.8 / 18.5   128 24.5 / 22.4
+//                    nucleus of 0.7  B = 1 25.6 / 21.7   64 29.5 / 28.1   128 30.3 / 31.5 (two parts: not taken)
+//   V = 152064 f32   plain           B = 32 32.8 / 14.2
+//                    nucleus of 0.7  B = 32 83 / 44      128 89 / 74 (two parts)
+//   V = 50003 bf16   plain           B = 32 14.7 / 16.1 (98 tiles: not taken)
+//                    nucleus of 0.7  B = 32 18.5 / 21.0 (not taken)
+//   V = 50003 f32    nucleus of 0.7  B = 16 36.3 / 30.9  64 37.1 / 35.8   100 38.2 / 39.2 (two parts: not taken)
+//   V = 32768 f32    plain           B = 4 11.5 / 10.3
+//                    top-k 50        B = 4 16.1 / 18.8 (two parts: not taken)
+// Greedy rows are read by one workgroup all the same.
 constexpr int64_t kComputeUnits = 256;
 enum Draws { kPlainDraws, kFilteredDraws, kNucleusDraws };  // without filters, with some, with top-p among them
 template <int DT>
