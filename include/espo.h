@@ -536,7 +536,8 @@ size_t espo_sample_workspace_bytes(int64_t B, int64_t V, espo_dtype dt);
  *   dlogits[n,v] = (g ([v = a] - pi_v) - h pi_v (ln pi_v + entropy[n])) / temperature
  * where g = dlogprob[n] and h = dentropy[n] are the loss's derivatives.  The sums are fp32, in an order that
  * follows the launch layout (which depends on N, V, the type and what is asked for, and on nothing else); a gradient is rounded to
- * the logits' type once, as it is stored.
+ * the logits' type once, as it is stored.  In a gradient, a weight e^t below 2^-125 may count as 0; where max x / temperature is beyond 10^7 on either
+ * side, whose exponents fp32 holds in coarser steps, below 2^-62.
  * A row whose token is outside [0, V) is not used (padding, a prompt): its logits are not read, logprob and entropy
  * are 0 and its gradient is 0.  Masked logits (at or below -1e30) have probability and gradient 0; a token that is
  * masked itself has logprob -inf.  (At temperatures above 1e20 this needs a largest logit above -1e29.)  NaN and +inf are not supported in rows that are used (results for that row are

@@ -23,7 +23,7 @@
 // What bounds it, and us a call on an MI355X at T = 1 where no other is named: large batches, LDS and double arithmetic per logit, not memory.
 // V = 152064 bf16, B = 512: plain, T = 0.6, 445 rows alive, 36 (135 MB at 3.7 TB/s; a look-up of 8 bytes per logit, 36 % of LDS's cycles conflicts),
 // nucleus of 0.7 60 (a count per logit besides, cut, second reading and draw).  Small ones, the chain of phases of one row: B = 64, settings of
-// all kinds, 36 (11 the parts' pass, 26 joining, cut and draw); B = 100, V = 50003 f32, the same, 55 (a mass takes a power of 2 in double and an addition of
+// all kinds, 36 (11 the parts' pass, 26 joining, cut and draw); B = 100, V = 50003 f32, the same, 55 to 59 (a mass takes a power of 2 in double and an addition of
 // 8 bytes in LDS, for each logit); B = 4, V = 32768 f32, plain 10.
 #include <hip/hip_runtime.h>
 #include <math.h>
